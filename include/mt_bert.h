@@ -466,6 +466,49 @@ int mt_kernel_pooler_head_static(const void* d_hidden, const void* d_pool_w, con
                                  int32_t batch, int32_t seq, int32_t hidden, int32_t num_classes,
                                  int32_t logits_stride, int32_t col0, void* stream);
 
+/* ---- the vocabulary's ends of a language model, and dropout ------------------------------------ */
+/* What the students that mt_load_weights takes are trained with (Section 3: fine-tuning of a task's own layers on frozen ones)
+ * and what scores a text by its tokens' probabilities, beside the forward pass.  As the steps above: device pointers, no model,
+ * asynchronous on `stream` of the current device, whose memory every pointer must be; nothing is allocated, nothing is kept
+ * between calls, any call can be captured into a CUDA graph.  Strides count elements from one row to the next (>= the row's
+ * length); rows themselves are contiguous.  A workspace is 256-byte aligned, of at least the size that its function gives, in
+ * use until the stream has passed the call, and holds nothing before or after it: calls that can run at the same time need one
+ * each.  Equal calls give equal bits: no sum depends on timing.
+ * Errors: UNSUPPORTED (a dtype that is none of those below), SHAPE (negative or too large sizes, strides below the row's
+ * length), INVALID_ARG (null or misaligned pointers, a workspace that is too small), CUDA. */
+#define MT_DTYPE_BF16 0
+#define MT_DTYPE_F32  1
+
+/* out[t, :] = scale * table[ids[t], :], tokens x hidden from a table [vocab, hidden], in fp32 and rounded once.  An id below 0
+ * is no token (a padded batch): its row of out is zeros.  So is that of an id >= vocab, which also sets MT_FLAG_BAD_TOKEN in
+ * *d_status (may be NULL).  Rows of 8 elements that are 16-byte aligned (hidden, strides multiples of 8) move fastest. */
+int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* d_out, int32_t tokens, int32_t vocab,
+                               int32_t hidden, int64_t table_stride, int64_t out_stride, int32_t table_dtype,
+                               int32_t out_dtype, float scale, uint32_t* d_status, void* stream);
+
+/* Gradient of the table: grad_table[v, :] = scale * sum over t with ids[t] = v of grad_out[t, :], summed in fp32 in an order
+ * that depends on the ids alone and rounded once; rows without a token become zeros.  accumulate != 0 adds to what grad_table
+ * holds instead, and leaves rows without a token alone.  Ids below 0 or >= vocab (flagged) have no part in it, nor has
+ * padding_id (< 0: there is none).  grad_out is not read at tokens that have no part.  tokens <= 2^30. */
+size_t mt_kernel_embedding_grad_workspace(int32_t tokens, int32_t vocab, int32_t hidden);
+int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void* d_grad_table, int32_t tokens, int32_t vocab,
+                             int32_t hidden, int64_t grad_out_stride, int64_t grad_table_stride, int32_t grad_out_dtype,
+                             int32_t grad_table_dtype, float scale, int32_t padding_id, int32_t accumulate, void* d_workspace,
+                             size_t workspace_bytes, uint32_t* d_status, void* stream);
+
+/* Dropout without a stored mask: y[r, c] = residual[r, c] + keep(r, c) * x[r, c] / (1 - q), q = p rounded to a multiple of
+ * 2^-16 (halves to even); residual may be NULL (0).  keep(r, c) is 0 where 16 random bits are below q * 2^16: half-word c % 8 of
+ * the Philox4x32-10 block (Salmon et al., 2011) with key `seed` and counter words (c / 8, r, low and high half of `counter`), so the
+ * mask depends on seed, counter, row and column alone, not on types or strides.  A caller takes another counter for every call
+ * of a step whose masks are to differ.  d_counter: NULL, or a device word that is added to `counter` (modulo 2^64) when the call
+ * runs - a replayed CUDA graph makes a new mask every time if something on its stream advances it.  The gradient with respect to
+ * x is this same call on the gradient of y, without a residual; that of the residual is the gradient of y.
+ * x has x_dtype, residual and y have y_dtype; y may be x or the residual itself, with the same stride.  p = 1 gives the residual.
+ * Dropped elements may be infinite or NaN. */
+int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_t rows, int32_t cols, int64_t x_stride,
+                      int64_t residual_stride, int64_t y_stride, int32_t x_dtype, int32_t y_dtype, double p, uint64_t seed,
+                      uint64_t counter, const uint64_t* d_counter, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ MT_OK = 0
 ERRORS = {0: "OK", -1: "INVALID_ARG", -2: "SHAPE", -3: "NOT_BOUND", -4: "NOT_LOADED", -5: "BLOB_MISMATCH",
           -6: "CUDA", -7: "UNSUPPORTED", -8: "DEVICE_FLAG"}
 FLAG_BAD_TOKEN, FLAG_BAD_SEGMENT, FLAG_BAD_LENGTH, FLAG_WAIT_TIMEOUT = 1, 2, 4, 8
+DTYPE_BF16, DTYPE_F32 = 0, 1
 KERNEL_CLASSES = ("embed", "qkv", "attention", "attn_out", "ln1", "ffn_up", "ffn_down", "ln2", "head", "quant")
 
 
@@ -33,7 +34,7 @@ class TaskConfig(C.Structure):
 
 
 # name -> (restype, argtypes); the list is also what the symbol-export test checks.
-_P, _I32, _U64, _SZ = C.c_void_p, C.c_int32, C.c_uint64, C.c_size_t
+_P, _I32, _I64, _U64, _SZ = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_size_t
 SIGNATURES = {
     "mt_create": (C.c_int, [C.POINTER(TrunkConfig), C.POINTER(TaskConfig), _I32, _I32, _I32, C.POINTER(_P)]),
     "mt_destroy": (None, [_P]),
@@ -76,6 +77,10 @@ SIGNATURES = {
                                   _P]),
     "mt_kernel_pooler_head": (C.c_int, [_P, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _P]),
     "mt_kernel_pooler_head_static": (C.c_int, [_P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _P]),
+    "mt_kernel_embedding_lookup": (C.c_int, [_P, _P, _P, _I32, _I32, _I32, _I64, _I64, _I32, _I32, C.c_float, _P, _P]),
+    "mt_kernel_embedding_grad_workspace": (_SZ, [_I32, _I32, _I32]),
+    "mt_kernel_embedding_grad": (C.c_int, [_P, _P, _P, _I32, _I32, _I32, _I64, _I64, _I32, _I32, C.c_float, _I32, _I32, _P, _SZ, _P, _P]),
+    "mt_kernel_dropout": (C.c_int, [_P, _P, _P, _I32, _I32, _I64, _I64, _I64, _I32, _I32, C.c_double, _U64, _U64, _P, _P]),
 }
 
 _lib = None
@@ -234,6 +239,105 @@ def mt_kernel_pooler_head_static(hidden, pool_w, pool_b, cls_w, cls_b, logits, b
     _check(lib().mt_kernel_pooler_head_static(_ptr(hidden), _ptr(pool_w), _ptr(pool_b), _ptr(cls_w), _ptr(cls_b),
                                               _ptr(logits), batch, seq, pool_w.shape[0], cls_w.shape[0],
                                               logits.shape[1], col0, _stream(stream)), "mt_kernel_pooler_head_static")
+
+
+# ---------------------------------------------------------------------------
+# the vocabulary's ends of a language model, and dropout
+# ---------------------------------------------------------------------------
+
+def _operands(where: str, *tensors) -> int:
+    """Refuses what the library cannot see: tensors that are not on the current device.  Returns that device's index."""
+    import torch
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise MTError(-1, where, f"a tensor is on {t.device}, the current device is cuda:{device}")
+    return device
+
+
+def _matrix(where: str, t, rows: int, cols: int):
+    """(pointer, dtype code, row stride) of a 2-D tensor with contiguous rows."""
+    import torch
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise MTError(-2, where, f"expected a {rows} x {cols} tensor, got {tuple(t.shape)}")
+    if t.dtype == torch.bfloat16:
+        dtype = DTYPE_BF16
+    elif t.dtype == torch.float32:
+        dtype = DTYPE_F32
+    else:
+        raise MTError(-7, where, f"dtype {t.dtype}")
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        raise MTError(-1, where, "the rows of a tensor are not contiguous")
+    # (the stride of a single row, or of none, says nothing)
+    return t.data_ptr(), dtype, stride if rows > 1 else max(stride, cols)
+
+
+def _vector(where: str, t, n: int, dtype: str) -> int:
+    """Pointer of a contiguous tensor of n elements of a type; 0 for None."""
+    if t is None:
+        return 0
+    if t.numel() != n or str(t.dtype) != "torch." + dtype or not t.is_contiguous():
+        raise MTError(-1, where, f"expected {n} contiguous {dtype} elements, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _stream_of(device: int, stream) -> int:
+    """The stream's handle; a stream of another device is refused."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    if stream.device.index != device:
+        raise MTError(-1, "stream", f"a stream of {stream.device}, the current device is cuda:{device}")
+    return stream.cuda_stream
+
+
+def mt_kernel_embedding_lookup(ids, table, out, scale: float = 1.0, status=None, stream=None) -> None:
+    """out[t] = scale * table[ids[t]] (ids int32 of any shape, out [ids.numel(), hidden]); zeros for ids < 0."""
+    where = "mt_kernel_embedding_lookup"
+    device = _operands(where, ids, table, out, status)
+    tokens, (vocab, hidden) = ids.numel(), table.shape
+    table_ptr, table_dtype, table_stride = _matrix(where, table, vocab, hidden)
+    out_ptr, out_dtype, out_stride = _matrix(where, out, tokens, hidden)
+    _check(lib().mt_kernel_embedding_lookup(_vector(where, ids, tokens, "int32"), table_ptr, out_ptr, tokens, vocab, hidden, table_stride,
+                                            out_stride, table_dtype, out_dtype, scale, _ptr(status), _stream_of(device, stream)), where)
+
+
+def mt_kernel_embedding_grad_workspace(tokens: int, vocab: int, hidden: int) -> int:
+    return lib().mt_kernel_embedding_grad_workspace(tokens, vocab, hidden)
+
+
+def mt_kernel_embedding_grad(ids, grad_out, grad_table, workspace, scale: float = 1.0, padding_id: int = -1,
+                             accumulate: bool = False, status=None, stream=None) -> None:
+    """grad_table[v] = scale * sum of grad_out[t] over ids[t] == v, zeros where there is none; or added to grad_table."""
+    where = "mt_kernel_embedding_grad"
+    device = _operands(where, ids, grad_out, grad_table, workspace, status)
+    tokens, (vocab, hidden) = ids.numel(), grad_table.shape
+    grad_ptr, grad_dtype, grad_stride = _matrix(where, grad_out, tokens, hidden)
+    table_ptr, table_dtype, table_stride = _matrix(where, grad_table, vocab, hidden)
+    _check(lib().mt_kernel_embedding_grad(_vector(where, ids, tokens, "int32"), grad_ptr, table_ptr, tokens, vocab, hidden, grad_stride,
+                                          table_stride, grad_dtype, table_dtype, scale, padding_id, 1 if accumulate else 0,
+                                          workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(status),
+                                          _stream_of(device, stream)), where)
+
+
+def mt_kernel_dropout(x, y, p: float, seed: int, counter: int = 0, residual=None, counter_dev=None, stream=None) -> None:
+    """y = residual + x * keep / (1 - p), keep from (seed, counter, row, column); ``counter_dev``: an int64 or uint64 device
+    tensor of one element that is added to ``counter`` when the call runs."""
+    where = "mt_kernel_dropout"
+    device = _operands(where, x, y, residual, counter_dev)
+    rows, cols = x.shape
+    x_ptr, x_dtype, x_stride = _matrix(where, x, rows, cols)
+    y_ptr, y_dtype, y_stride = _matrix(where, y, rows, cols)
+    r_ptr, r_stride = 0, 0
+    if residual is not None:
+        r_ptr, r_dtype, r_stride = _matrix(where, residual, rows, cols)
+        if r_dtype != y_dtype:
+            raise MTError(-1, where, "residual and y have different types")
+    if counter_dev is not None and (counter_dev.numel() != 1 or counter_dev.element_size() != 8 or counter_dev.is_floating_point()):
+        raise MTError(-1, where, "counter_dev is one 64-bit integer")
+    _check(lib().mt_kernel_dropout(x_ptr, r_ptr, y_ptr, rows, cols, x_stride, r_stride, y_stride, x_dtype, y_dtype, p,
+                                   seed & 0xFFFFFFFFFFFFFFFF, counter & 0xFFFFFFFFFFFFFFFF, _ptr(counter_dev), _stream_of(device, stream)), where)
 
 
 # ---------------------------------------------------------------------------

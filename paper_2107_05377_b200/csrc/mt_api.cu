@@ -2423,4 +2423,104 @@ int mt_kernel_pooler_head(const void* d_hidden, const void* d_pool_w, const void
   return launch_pooler_head(p, as_stream(stream)) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 
+// ---- the vocabulary's ends of a language model, and dropout --------------------------------------
+
+static bool known_dtype(int32_t dtype) { return dtype == MT_DTYPE_BF16 || dtype == MT_DTYPE_F32; }
+static bool misaligned(const void* p, int32_t dtype) { return reinterpret_cast<uintptr_t>(p) % (dtype == MT_DTYPE_F32 ? 4 : 2) != 0; }
+static constexpr int32_t kMaxTokens = 1 << 30;
+
+// SMs of the current device (MT_ERR_CUDA without one).
+static int current_sms(int* sms) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return MT_ERR_CUDA;
+  return MT_OK;
+}
+static size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* d_out, int32_t tokens, int32_t vocab, int32_t hidden,
+                               int64_t table_stride, int64_t out_stride, int32_t table_dtype, int32_t out_dtype, float scale,
+                               uint32_t* d_status, void* stream) {
+  if (!known_dtype(table_dtype) || !known_dtype(out_dtype)) return MT_ERR_UNSUPPORTED;
+  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || table_stride < hidden || out_stride < hidden) return MT_ERR_SHAPE;
+  if (tokens == 0) return MT_OK;
+  if (d_ids == nullptr || d_table == nullptr || d_out == nullptr || reinterpret_cast<uintptr_t>(d_ids) % 4 != 0 ||
+      misaligned(d_table, table_dtype) || misaligned(d_out, out_dtype))
+    return MT_ERR_INVALID_ARG;
+  int sms = 0;
+  if (current_sms(&sms) != MT_OK) return MT_ERR_CUDA;
+  LookupParams p;
+  p.ids = d_ids; p.table = d_table; p.out = d_out; p.table_stride = table_stride; p.out_stride = out_stride;
+  p.tokens = tokens; p.vocab = vocab; p.hidden = hidden; p.scale = scale; p.status = d_status;
+  return launch_embedding_lookup(p, table_dtype == MT_DTYPE_F32, out_dtype == MT_DTYPE_F32, sms, as_stream(stream)) == cudaSuccess
+             ? MT_OK : MT_ERR_CUDA;
+}
+
+// Workspace: four lists of the tokens, then the parts of every chunk.
+static size_t embedding_list_bytes(int32_t tokens) { return whole_lines(static_cast<size_t>(tokens) * 4); }
+static int64_t embedding_part_stride(int32_t hidden) { return (static_cast<int64_t>(hidden) + 7) / 8 * 8; }
+
+size_t mt_kernel_embedding_grad_workspace(int32_t tokens, int32_t vocab, int32_t hidden) {
+  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1) return 0;
+  if (tokens == 0) return 256;
+  const int chunk = embedding_grad_chunk(tokens);
+  const size_t chunks = (static_cast<size_t>(tokens) + chunk - 1) / chunk;
+  return 4 * embedding_list_bytes(tokens) + whole_lines(chunks * 2 * embedding_part_stride(hidden) * 4);
+}
+
+int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void* d_grad_table, int32_t tokens, int32_t vocab,
+                             int32_t hidden, int64_t grad_out_stride, int64_t grad_table_stride, int32_t grad_out_dtype,
+                             int32_t grad_table_dtype, float scale, int32_t padding_id, int32_t accumulate, void* d_workspace,
+                             size_t workspace_bytes, uint32_t* d_status, void* stream) {
+  if (!known_dtype(grad_out_dtype) || !known_dtype(grad_table_dtype)) return MT_ERR_UNSUPPORTED;
+  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || grad_out_stride < hidden || grad_table_stride < hidden)
+    return MT_ERR_SHAPE;
+  if (d_grad_table == nullptr || misaligned(d_grad_table, grad_table_dtype)) return MT_ERR_INVALID_ARG;
+  if (tokens > 0 && (d_ids == nullptr || d_grad_out == nullptr || reinterpret_cast<uintptr_t>(d_ids) % 4 != 0 ||
+                     misaligned(d_grad_out, grad_out_dtype) || d_workspace == nullptr || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
+                     workspace_bytes < mt_kernel_embedding_grad_workspace(tokens, vocab, hidden)))
+    return MT_ERR_INVALID_ARG;
+  if (tokens == 0 && accumulate != 0) return MT_OK;
+  int sms = 0;
+  if (current_sms(&sms) != MT_OK) return MT_ERR_CUDA;
+  EmbeddingGradParams p;
+  memset(&p, 0, sizeof(p));
+  p.ids = d_ids; p.grad_out = d_grad_out; p.grad_table = d_grad_table;
+  p.grad_stride = grad_out_stride; p.table_stride = grad_table_stride;
+  p.tokens = tokens; p.vocab = vocab; p.hidden = hidden; p.scale = scale; p.status = d_status;
+  p.padding_id = padding_id < 0 ? -1 : padding_id; p.accumulate = accumulate != 0 ? 1 : 0;
+  uint8_t* ws = static_cast<uint8_t*>(d_workspace);
+  for (int i = 0; i < 2; ++i) {
+    p.keys[i] = reinterpret_cast<uint32_t*>(ws + (2 * i) * embedding_list_bytes(tokens));
+    p.order[i] = reinterpret_cast<uint32_t*>(ws + (2 * i + 1) * embedding_list_bytes(tokens));
+  }
+  p.parts = reinterpret_cast<float*>(ws + 4 * embedding_list_bytes(tokens));
+  p.part_stride = embedding_part_stride(hidden);
+  p.chunk = embedding_grad_chunk(tokens);
+  return launch_embedding_grad(p, grad_out_dtype == MT_DTYPE_F32, grad_table_dtype == MT_DTYPE_F32, sms, as_stream(stream)) == cudaSuccess
+             ? MT_OK : MT_ERR_CUDA;
+}
+
+int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_t rows, int32_t cols, int64_t x_stride,
+                      int64_t residual_stride, int64_t y_stride, int32_t x_dtype, int32_t y_dtype, double p_drop, uint64_t seed,
+                      uint64_t counter, const uint64_t* d_counter, void* stream) {
+  if (!known_dtype(x_dtype) || !known_dtype(y_dtype)) return MT_ERR_UNSUPPORTED;
+  if (!(p_drop >= 0.0 && p_drop <= 1.0)) return MT_ERR_INVALID_ARG;
+  if (rows < 0 || cols < 0 || x_stride < cols || y_stride < cols || (d_residual != nullptr && residual_stride < cols)) return MT_ERR_SHAPE;
+  if (rows == 0 || cols == 0) return MT_OK;
+  if (d_x == nullptr || d_y == nullptr || misaligned(d_x, x_dtype) || misaligned(d_y, y_dtype) || misaligned(d_residual, y_dtype) ||
+      reinterpret_cast<uintptr_t>(d_counter) % 8 != 0)
+    return MT_ERR_INVALID_ARG;
+  int sms = 0;
+  if (current_sms(&sms) != MT_OK) return MT_ERR_CUDA;
+  DropoutParams p;
+  memset(&p, 0, sizeof(p));
+  p.x = d_x; p.residual = d_residual; p.y = d_y;
+  p.x_stride = x_stride; p.residual_stride = residual_stride; p.y_stride = y_stride;
+  p.rows = rows; p.cols = cols; p.seed = seed; p.counter = counter; p.counter_dev = d_counter;
+  p.threshold = static_cast<uint32_t>(nearbyint(p_drop * 65536.0));      // (halves to the even neighbour)
+  p.factor = p.threshold == 65536u ? 0.f : static_cast<float>(65536.0 / (65536.0 - p.threshold));
+  return launch_dropout(p, x_dtype == MT_DTYPE_F32, y_dtype == MT_DTYPE_F32, sms, as_stream(stream)) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+}
+
 }  // extern "C"

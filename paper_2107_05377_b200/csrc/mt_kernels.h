@@ -390,4 +390,56 @@ cudaError_t launch_pooler_head(const HeadParams& p, cudaStream_t stream);   // b
 // The head alone, for a caller that has filled `pooled` itself (the pooler as a grouped GEMM).
 cudaError_t launch_head(const HeadParams& p, cudaStream_t stream);
 
+// ---- the vocabulary's ends of a language model, and dropout ------------------------------------
+
+// out[t, :] = scale * table[ids[t], :]; rows of zeros for ids < 0 and, flagged, for ids >= vocab.  Strides in elements.
+struct LookupParams {
+  const int32_t* ids;
+  const void* table;
+  void* out;
+  int64_t table_stride, out_stride;
+  int32_t tokens, vocab, hidden;
+  float scale;
+  uint32_t* status;
+};
+cudaError_t launch_embedding_lookup(const LookupParams& p, bool table_f32, bool out_f32, int sm_count, cudaStream_t stream);
+
+// grad_table[v, :] (+)= scale * sum over ids[t] = v of grad_out[t, :]; up to three launches (sort, sum, join).
+constexpr int kEmbeddingMaxChunk = 1024;   // sorted entries of a CTA of the sum, at most
+struct EmbeddingGradParams {
+  const int32_t* ids;
+  const void* grad_out;
+  void* grad_table;
+  int64_t grad_stride, table_stride;
+  int32_t tokens, vocab, hidden;
+  int32_t padding_id;       // row without a gradient (-1: none)
+  int32_t accumulate;
+  float scale;
+  uint32_t* status;
+  // workspace: the sorted list, written in turn, and what chunks have of runs that cross their borders ([chunk][2][part_stride])
+  uint32_t* keys[2];
+  uint32_t* order[2];
+  float* parts;
+  int64_t part_stride;
+  int32_t chunk;            // embedding_grad_chunk(tokens)
+  // chosen by the launcher
+  int32_t passes, digit_bits, sort_ctas, vectors;
+};
+int embedding_grad_chunk(int tokens);
+cudaError_t launch_embedding_grad(EmbeddingGradParams p, bool grad_f32, bool out_f32, int sm_count, cudaStream_t stream);
+
+// y = residual + x * keep / (1 - p) with keep from a counter-based generator; threshold = p * 65536, factor = 1 / (1 - p).
+struct DropoutParams {
+  const void* x;
+  const void* residual;     // or null
+  void* y;
+  int64_t x_stride, residual_stride, y_stride;
+  int32_t rows, cols;
+  uint32_t threshold;
+  float factor;
+  uint64_t seed, counter;
+  const uint64_t* counter_dev;   // or null: added to `counter`
+};
+cudaError_t launch_dropout(const DropoutParams& p, bool x_f32, bool y_f32, int sm_count, cudaStream_t stream);
+
 }  // namespace mt

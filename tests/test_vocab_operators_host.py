@@ -1,0 +1,62 @@
+"""Refusals of the vocabulary operators and of dropout that need no GPU: every check comes before the first CUDA call."""
+import pytest
+
+from paper_2107_05377_b200 import binding, build
+
+INVALID, SHAPE, CUDA, UNSUPPORTED = -1, -2, -6, -7
+A = 1 << 20            # stands for a device address; nothing reads it
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return binding.lib()
+
+
+LOOKUP = dict(ids=A, table=A, out=A, tokens=4, vocab=9, hidden=16, table_stride=16, out_stride=16, table_dtype=0, out_dtype=1, scale=1.0,
+              status=0, stream=0)
+GRAD = dict(ids=A, grad=A, table=A, tokens=4, vocab=9, hidden=16, grad_stride=16, table_stride=16, grad_dtype=0, table_dtype=1, scale=1.0,
+            padding=-1, accumulate=0, ws=A, ws_bytes=1 << 20, status=0, stream=0)
+DROPOUT = dict(x=A, residual=0, y=A, rows=4, cols=16, x_stride=16, residual_stride=0, y_stride=16, x_dtype=0, y_dtype=1, p=0.1, seed=1, counter=2,
+               counter_dev=0, stream=0)
+
+
+def call(lib, name, base, **change):
+    return getattr(lib, name)(*(base | change).values())
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(table_dtype=2), UNSUPPORTED), (dict(out_dtype=-1), UNSUPPORTED), (dict(tokens=-1), SHAPE), (dict(tokens=(1 << 30) + 1), SHAPE),
+    (dict(vocab=0), SHAPE), (dict(hidden=0), SHAPE), (dict(table_stride=15), SHAPE), (dict(out_stride=-16), SHAPE), (dict(ids=0), INVALID),
+    (dict(table=0), INVALID), (dict(out=0), INVALID), (dict(ids=A + 2), INVALID), (dict(table=A + 1), INVALID), (dict(out=A + 2), INVALID),
+    (dict(tokens=0, ids=0, table=0, out=0), 0)])
+def test_lookup(lib, change, want):
+    assert call(lib, "mt_kernel_embedding_lookup", LOOKUP, **change) == want
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(grad_dtype=2), UNSUPPORTED), (dict(table_dtype=7), UNSUPPORTED), (dict(tokens=-1), SHAPE), (dict(tokens=(1 << 30) + 1), SHAPE),
+    (dict(vocab=-4), SHAPE), (dict(hidden=0), SHAPE), (dict(grad_stride=8), SHAPE), (dict(table_stride=8), SHAPE), (dict(ids=0), INVALID),
+    (dict(grad=0), INVALID), (dict(table=0), INVALID), (dict(ws=0), INVALID), (dict(ws=A + 16), INVALID), (dict(ws_bytes=255), INVALID),
+    (dict(grad=A + 1), INVALID), (dict(table=A + 2), INVALID), (dict(tokens=0, accumulate=1, ids=0, grad=0, ws=0), 0)])
+def test_gradient(lib, change, want):
+    assert call(lib, "mt_kernel_embedding_grad", GRAD, **change) == want
+
+
+def test_gradient_workspace(lib):
+    size = lib.mt_kernel_embedding_grad_workspace
+    assert size(-1, 9, 16) == 0 and size(4, 0, 16) == 0 and size(4, 9, 0) == 0 and size((1 << 30) + 1, 9, 16) == 0
+    assert size(0, 9, 16) >= 1
+    for tokens in (1, 7, 8, 9, 4096, 131072, 1 << 30):
+        chunks = size(tokens, 9, 8) - 4 * ((tokens * 4 + 255) // 256 * 256)
+        assert chunks % 256 == 0 and chunks > 0
+    assert size(1 << 30, 9, 1024) > 1 << 33            # (counted in 64 bits)
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(x_dtype=2), UNSUPPORTED), (dict(y_dtype=-3), UNSUPPORTED), (dict(p=-0.01), INVALID), (dict(p=1.01), INVALID), (dict(p=float("nan")), INVALID),
+    (dict(rows=-1), SHAPE), (dict(cols=-1), SHAPE), (dict(x_stride=15), SHAPE), (dict(y_stride=0), SHAPE), (dict(residual=A, residual_stride=4), SHAPE),
+    (dict(x=0), INVALID), (dict(y=0), INVALID), (dict(x=A + 1), INVALID), (dict(y=A + 2), INVALID), (dict(residual=A + 2, residual_stride=16), INVALID),
+    (dict(counter_dev=A + 4), INVALID), (dict(rows=0, x=0, y=0), 0), (dict(cols=0, x=0, y=0), 0)])
+def test_dropout(lib, change, want):
+    assert call(lib, "mt_kernel_dropout", DROPOUT, **change) == want
