@@ -509,6 +509,28 @@ int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_
                       int64_t residual_stride, int64_t y_stride, int32_t x_dtype, int32_t y_dtype, double p, uint64_t seed,
                       uint64_t counter, const uint64_t* d_counter, void* stream);
 
+/* Softmax cross entropy over a vocabulary, the logits never kept:
+ *   z = x W^T + bias,  lse[n] = log sum_v exp z[n, v],  loss[n] = lse[n] - z[n, labels[n]]
+ * x [rows, hidden], W [vocab, hidden] and bias [vocab] (or NULL) bf16, loss and lse fp32 [rows]; sums in fp32 on tcgen05.  A row whose
+ * label is below 0 takes no part (what x holds there has no influence): loss and lse are 0 there; so does one whose label is
+ * >= vocab, which sets MT_FLAG_BAD_TOKEN.  A bias of -inf bans a word.  hidden % 8 == 0, 8 .. 16384; rows, vocab <= 2^22; strides
+ * multiples of 8; x, W and bias 16-byte aligned.  With more than 256 rows the work is that of the rows with a label. */
+size_t mt_kernel_vocab_loss_workspace(int32_t rows, int32_t vocab, int32_t hidden);
+int mt_kernel_vocab_loss(const void* d_x, const void* d_w, const void* d_bias, const int32_t* d_labels, float* d_loss, float* d_lse,
+                         int32_t rows, int32_t vocab, int32_t hidden, int64_t x_stride, int64_t w_stride, void* d_workspace,
+                         size_t workspace_bytes, uint32_t* d_status, void* stream);
+/* Gradients of sum_n grad_loss[n] * loss[n] (grad_loss fp32 [rows], NULL: ones), with the lse of mt_kernel_vocab_loss:
+ *   g = grad_loss (exp(z - lse) - onehot(label)),  grad_x = g W,  grad_w = g^T x,  grad_bias = sum over rows of g
+ * grad_x [rows, hidden] and grad_w [vocab, hidden] bf16, grad_bias [vocab] fp32; any two of them may be NULL (a frozen trunk, a frozen
+ * table).  The logits are made again, a piece of the vocabulary at a time; g is rounded to bf16 as the operand of the two products
+ * (grad_bias is summed from it before that), which sum in fp32 and round once.  accumulate != 0 adds grad_w and grad_bias to what is
+ * there.  Rows without a label: zeros in grad_x, no part in the others.  Sizes and alignment as above. */
+size_t mt_kernel_vocab_loss_grad_workspace(int32_t rows, int32_t vocab, int32_t hidden);
+int mt_kernel_vocab_loss_grad(const void* d_x, const void* d_w, const void* d_bias, const int32_t* d_labels, const float* d_lse,
+                              const float* d_grad_loss, void* d_grad_x, void* d_grad_w, float* d_grad_bias, int32_t rows, int32_t vocab,
+                              int32_t hidden, int64_t x_stride, int64_t w_stride, int64_t grad_x_stride, int64_t grad_w_stride,
+                              int32_t accumulate, void* d_workspace, size_t workspace_bytes, uint32_t* d_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

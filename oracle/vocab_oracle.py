@@ -65,29 +65,33 @@ def embedding_grad(ids, grad_out, vocab, scale=1.0, padding_id=-1):
     return scale * total, abs(scale) * size, count
 
 
+def _softmax_rows(x, w, bias, labels, block=512):
+    """For blocks of rows with a label (0 <= label < vocab): the rows, their labels, logits and log-sum-exp."""
+    labels = np.asarray(labels)
+    rows = np.flatnonzero((labels >= 0) & (labels < len(w)))
+    for at in (rows[i:i + block] for i in range(0, len(rows), block)):
+        z = x[at] @ w.T + (0.0 if bias is None else bias)
+        top = z.max(axis=1)
+        yield at, labels[at], z, top + np.log(np.exp(z - top[:, None]).sum(axis=1))
+
+
 def vocab_loss(x, w, bias, labels):
-    """loss and log-sum-exp of every row with a label (0 <= label < vocab); zeros elsewhere."""
+    """loss and log-sum-exp of every row with a label; zeros elsewhere."""
     loss, lse = np.zeros(len(x)), np.zeros(len(x))
-    for n, label in enumerate(labels):
-        if 0 <= label < len(w):
-            z = w @ x[n] + (0.0 if bias is None else bias)
-            top = z.max()
-            lse[n] = top + np.log(np.exp(z - top).sum())
-            loss[n] = lse[n] - z[label]
+    for at, label, z, total in _softmax_rows(x, w, bias, labels):
+        lse[at] = total
+        loss[at] = total - z[np.arange(len(at)), label]
     return loss, lse
 
 
 def vocab_loss_grad(x, w, bias, labels, grad_loss):
     """Gradients of sum_n grad_loss[n] * loss[n] with respect to x, w and bias."""
     dx, dw, db = np.zeros(x.shape), np.zeros(w.shape), np.zeros(len(w))
-    for n, label in enumerate(labels):
-        if 0 <= label < len(w):
-            z = w @ x[n] + (0.0 if bias is None else bias)
-            p = np.exp(z - z.max())
-            g = p / p.sum()
-            g[label] -= 1.0
-            g *= grad_loss[n]
-            dx[n] = g @ w
-            dw += np.outer(g, x[n])
-            db += g
+    for at, label, z, total in _softmax_rows(x, w, bias, labels):
+        g = np.exp(z - total[:, None])
+        g[np.arange(len(at)), label] -= 1.0
+        g *= grad_loss[at][:, None]
+        dx[at] = g @ w
+        dw += g.T @ x[at]
+        db += g.sum(axis=0)
     return dx, dw, db

@@ -81,6 +81,11 @@ SIGNATURES = {
     "mt_kernel_embedding_grad_workspace": (_SZ, [_I32, _I32, _I32]),
     "mt_kernel_embedding_grad": (C.c_int, [_P, _P, _P, _I32, _I32, _I32, _I64, _I64, _I32, _I32, C.c_float, _I32, _I32, _P, _SZ, _P, _P]),
     "mt_kernel_dropout": (C.c_int, [_P, _P, _P, _I32, _I32, _I64, _I64, _I64, _I32, _I32, C.c_double, _U64, _U64, _P, _P]),
+    "mt_kernel_vocab_loss_workspace": (_SZ, [_I32, _I32, _I32]),
+    "mt_kernel_vocab_loss": (C.c_int, [_P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I64, _I64, _P, _SZ, _P, _P]),
+    "mt_kernel_vocab_loss_grad_workspace": (_SZ, [_I32, _I32, _I32]),
+    "mt_kernel_vocab_loss_grad": (C.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I64, _I64, _I64, _I64, _I32, _P, _SZ, _P,
+                                            _P]),
 }
 
 _lib = None
@@ -338,6 +343,53 @@ def mt_kernel_dropout(x, y, p: float, seed: int, counter: int = 0, residual=None
         raise MTError(-1, where, "counter_dev is one 64-bit integer")
     _check(lib().mt_kernel_dropout(x_ptr, r_ptr, y_ptr, rows, cols, x_stride, r_stride, y_stride, x_dtype, y_dtype, p,
                                    seed & 0xFFFFFFFFFFFFFFFF, counter & 0xFFFFFFFFFFFFFFFF, _ptr(counter_dev), _stream_of(device, stream)), where)
+
+
+def _bf16_matrix(where: str, t, rows: int, cols: int):
+    pointer, dtype, stride = _matrix(where, t, rows, cols)
+    if dtype != DTYPE_BF16:
+        raise MTError(-7, where, f"dtype {t.dtype}")
+    # (nobody walks the stride of a single row: any that the library takes will do)
+    return pointer, stride if rows > 1 else cols
+
+
+def mt_kernel_vocab_loss_workspace(rows: int, vocab: int, hidden: int) -> int:
+    return lib().mt_kernel_vocab_loss_workspace(rows, vocab, hidden)
+
+
+def mt_kernel_vocab_loss(x, w, bias, labels, loss, lse, workspace, status=None, stream=None) -> None:
+    """loss[n] = lse[n] - z[n, labels[n]], lse = log sum exp z, z = x w^T + bias; both 0 where labels[n] < 0."""
+    where = "mt_kernel_vocab_loss"
+    device = _operands(where, x, w, bias, labels, loss, lse, workspace, status)
+    (rows, hidden), vocab = x.shape, w.shape[0]
+    x_ptr, x_stride = _bf16_matrix(where, x, rows, hidden)
+    w_ptr, w_stride = _bf16_matrix(where, w, vocab, hidden)
+    _check(lib().mt_kernel_vocab_loss(x_ptr, w_ptr, _vector(where, bias, vocab, "bfloat16"), _vector(where, labels, rows, "int32"),
+                                      _vector(where, loss, rows, "float32"), _vector(where, lse, rows, "float32"), rows, vocab, hidden,
+                                      x_stride, w_stride, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(status),
+                                      _stream_of(device, stream)), where)
+
+
+def mt_kernel_vocab_loss_grad_workspace(rows: int, vocab: int, hidden: int) -> int:
+    return lib().mt_kernel_vocab_loss_grad_workspace(rows, vocab, hidden)
+
+
+def mt_kernel_vocab_loss_grad(x, w, bias, labels, lse, grad_loss, grad_x, grad_w, grad_bias, workspace, accumulate: bool = False, status=None,
+                              stream=None) -> None:
+    """Gradients of (grad_loss * loss).sum(); grad_loss None stands for ones, a gradient that is None is not taken.  ``accumulate``
+    adds to grad_w and grad_bias."""
+    where = "mt_kernel_vocab_loss_grad"
+    device = _operands(where, x, w, bias, labels, lse, grad_loss, grad_x, grad_w, grad_bias, workspace, status)
+    (rows, hidden), vocab = x.shape, w.shape[0]
+    x_ptr, x_stride = _bf16_matrix(where, x, rows, hidden)
+    w_ptr, w_stride = _bf16_matrix(where, w, vocab, hidden)
+    dx_ptr, dx_stride = _bf16_matrix(where, grad_x, rows, hidden) if grad_x is not None else (0, hidden)
+    dw_ptr, dw_stride = _bf16_matrix(where, grad_w, vocab, hidden) if grad_w is not None else (0, hidden)
+    _check(lib().mt_kernel_vocab_loss_grad(x_ptr, w_ptr, _vector(where, bias, vocab, "bfloat16"), _vector(where, labels, rows, "int32"),
+                                           _vector(where, lse, rows, "float32"), _vector(where, grad_loss, rows, "float32"), dx_ptr, dw_ptr,
+                                           _vector(where, grad_bias, vocab, "float32"), rows, vocab, hidden, x_stride, w_stride, dx_stride,
+                                           dw_stride, 1 if accumulate else 0, workspace.data_ptr(),
+                                           workspace.numel() * workspace.element_size(), _ptr(status), _stream_of(device, stream)), where)
 
 
 # ---------------------------------------------------------------------------

@@ -12,7 +12,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmt_bert.so")
-SOURCES = ["mt_api.cu", "gemm_tcgen05.cu", "attention.cu", "cls_pool.cu", "attention_tc.cu", "qkv_attention_tcgen05.cu", "gemm_ln_tcgen05.cu", "gemm_ln_pair_tcgen05.cu", "gemm_ln_low_tcgen05.cu", "gemm_low_tcgen05.cu", "rowwise.cu", "noalloc.cu", "wait_probe.cu", "embedding.cu", "dropout.cu"]
+SOURCES = ["mt_api.cu", "gemm_tcgen05.cu", "attention.cu", "cls_pool.cu", "attention_tc.cu", "qkv_attention_tcgen05.cu", "gemm_ln_tcgen05.cu", "gemm_ln_pair_tcgen05.cu", "gemm_ln_low_tcgen05.cu", "gemm_low_tcgen05.cu", "rowwise.cu", "noalloc.cu", "wait_probe.cu", "embedding.cu", "dropout.cu", "vocab_loss.cu"]
 
 
 def sources():

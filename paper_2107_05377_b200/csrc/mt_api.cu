@@ -265,20 +265,22 @@ cudaError_t get_encoder(EncodeTiledFn* out) {
 // Tensor map of a row-major matrix [rows, cols] (bf16, or fp32 when `fp32`) accessed in boxes of
 // box_rows x box_cols whose rows are 128 bytes, with the 128-byte swizzle; out-of-range parts of a
 // box read as zero and are skipped on stores.
-cudaError_t make_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows, int box_cols,
-                      bool fp32) {
+cudaError_t make_tmap_strided(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_cols,
+                              bool fp32) {
   EncodeTiledFn enc = nullptr;
   cudaError_t err = get_encoder(&enc);
   if (err != cudaSuccess) return err;
-  const size_t elem_bytes = fp32 ? sizeof(float) : sizeof(bf16);
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols) * elem_bytes};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(row_bytes)};
   const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)};
   const cuuint32_t elem[2] = {1, 1};
   CUresult r = enc(map, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
                    const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+cudaError_t make_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows, int box_cols, bool fp32) {
+  return make_tmap_strided(map, base, rows, cols, cols * static_cast<int64_t>(fp32 ? sizeof(float) : sizeof(bf16)), box_rows, box_cols, fp32);
 }
 
 // Tensor map of a row-major bf16 matrix [rows, cols] as {64, rows, cols / 64}: a box is some rows of several k-blocks, one
@@ -2436,6 +2438,11 @@ static int current_sms(int* sms) {
     return MT_ERR_CUDA;
   return MT_OK;
 }
+// Sizes whose tiles are counted in 32 bits; hidden and strides so that every row is 16-byte aligned (TMA).
+static bool vocab_sizes_ok(int32_t rows, int32_t vocab, int32_t hidden) {
+  return rows >= 0 && rows <= 1 << 22 && vocab >= 1 && vocab <= 1 << 22 && hidden >= 8 && hidden <= 1 << 14 && hidden % 8 == 0;
+}
+static bool vocab_stride_ok(int64_t stride, int32_t hidden) { return stride >= hidden && stride % 8 == 0 && stride < (int64_t{1} << 38); }
 static size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* d_out, int32_t tokens, int32_t vocab, int32_t hidden,
@@ -2523,4 +2530,73 @@ int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_
   return launch_dropout(p, x_dtype == MT_DTYPE_F32, y_dtype == MT_DTYPE_F32, sms, as_stream(stream)) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 
+size_t mt_kernel_vocab_loss_workspace(int32_t rows, int32_t vocab, int32_t hidden) {
+  return vocab_sizes_ok(rows, vocab, hidden) ? vocab_loss_workspace(rows, vocab, hidden) : 0;
+}
+size_t mt_kernel_vocab_loss_grad_workspace(int32_t rows, int32_t vocab, int32_t hidden) {
+  return vocab_sizes_ok(rows, vocab, hidden) ? vocab_loss_grad_workspace(rows, vocab, hidden) : 0;
+}
+
+int mt_kernel_vocab_loss(const void* d_x, const void* d_w, const void* d_bias, const int32_t* d_labels, float* d_loss, float* d_lse,
+                         int32_t rows, int32_t vocab, int32_t hidden, int64_t x_stride, int64_t w_stride, void* d_workspace,
+                         size_t workspace_bytes, uint32_t* d_status, void* stream) {
+  if (!vocab_sizes_ok(rows, vocab, hidden) || !vocab_stride_ok(x_stride, hidden) || !vocab_stride_ok(w_stride, hidden)) return MT_ERR_SHAPE;
+  if (rows == 0) return MT_OK;
+  if (d_x == nullptr || d_w == nullptr || d_labels == nullptr || d_loss == nullptr || d_lse == nullptr || d_workspace == nullptr ||
+      misaligned16({d_x, d_w, d_bias}) || misaligned(d_labels, MT_DTYPE_F32) || misaligned(d_loss, MT_DTYPE_F32) ||
+      misaligned(d_lse, MT_DTYPE_F32) || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
+      workspace_bytes < mt_kernel_vocab_loss_workspace(rows, vocab, hidden))
+    return MT_ERR_INVALID_ARG;
+  int sms = 0;
+  if (current_sms(&sms) != MT_OK) return MT_ERR_CUDA;
+  VocabLossCall c;
+  memset(&c, 0, sizeof(c));
+  c.x = static_cast<const bf16*>(d_x); c.w = static_cast<const bf16*>(d_w); c.bias = static_cast<const bf16*>(d_bias);
+  c.labels = d_labels; c.x_stride = x_stride; c.w_stride = w_stride; c.rows = rows; c.vocab = vocab; c.hidden = hidden;
+  c.status = d_status; c.workspace = d_workspace; c.loss = d_loss; c.lse_out = d_lse;
+  return launch_vocab_loss(c, sms, as_stream(stream)) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+}
+
+int mt_kernel_vocab_loss_grad(const void* d_x, const void* d_w, const void* d_bias, const int32_t* d_labels, const float* d_lse,
+                              const float* d_grad_loss, void* d_grad_x, void* d_grad_w, float* d_grad_bias, int32_t rows, int32_t vocab,
+                              int32_t hidden, int64_t x_stride, int64_t w_stride, int64_t grad_x_stride, int64_t grad_w_stride,
+                              int32_t accumulate, void* d_workspace, size_t workspace_bytes, uint32_t* d_status, void* stream_) {
+  if (!vocab_sizes_ok(rows, vocab, hidden) || !vocab_stride_ok(x_stride, hidden) || !vocab_stride_ok(w_stride, hidden) ||
+      (d_grad_x != nullptr && !vocab_stride_ok(grad_x_stride, hidden)) || (d_grad_w != nullptr && !vocab_stride_ok(grad_w_stride, hidden)))
+    return MT_ERR_SHAPE;
+  if ((d_grad_x == nullptr && d_grad_w == nullptr && d_grad_bias == nullptr) || misaligned16({d_grad_x, d_grad_w}) ||
+      misaligned(d_grad_bias, MT_DTYPE_F32))
+    return MT_ERR_INVALID_ARG;
+  cudaStream_t stream = as_stream(stream_);
+  if (rows == 0) {
+    if (accumulate != 0) return MT_OK;
+    if (d_grad_w != nullptr && cudaMemset2DAsync(d_grad_w, grad_w_stride * 2, 0, static_cast<size_t>(hidden) * 2, vocab, stream) != cudaSuccess)
+      return MT_ERR_CUDA;
+    if (d_grad_bias != nullptr && cudaMemsetAsync(d_grad_bias, 0, static_cast<size_t>(vocab) * 4, stream) != cudaSuccess) return MT_ERR_CUDA;
+    return MT_OK;
+  }
+  if (d_x == nullptr || d_w == nullptr || d_labels == nullptr || d_lse == nullptr || d_workspace == nullptr ||
+      misaligned16({d_x, d_w, d_bias}) || misaligned(d_labels, MT_DTYPE_F32) || misaligned(d_lse, MT_DTYPE_F32) ||
+      misaligned(d_grad_loss, MT_DTYPE_F32) || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
+      workspace_bytes < mt_kernel_vocab_loss_grad_workspace(rows, vocab, hidden))
+    return MT_ERR_INVALID_ARG;
+  int sms = 0;
+  if (current_sms(&sms) != MT_OK) return MT_ERR_CUDA;
+  VocabLossCall c;
+  memset(&c, 0, sizeof(c));
+  c.x = static_cast<const bf16*>(d_x); c.w = static_cast<const bf16*>(d_w); c.bias = static_cast<const bf16*>(d_bias);
+  c.labels = d_labels; c.x_stride = x_stride; c.w_stride = w_stride; c.rows = rows; c.vocab = vocab; c.hidden = hidden;
+  c.status = d_status; c.workspace = d_workspace; c.lse = d_lse; c.grad_loss = d_grad_loss;
+  c.dx = static_cast<bf16*>(d_grad_x); c.dw = static_cast<bf16*>(d_grad_w); c.db = d_grad_bias;
+  c.dx_stride = grad_x_stride; c.dw_stride = grad_w_stride; c.accumulate = accumulate != 0 ? 1 : 0;
+  return launch_vocab_loss_grad(c, sms, stream) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+}
+
 }  // extern "C"
+
+namespace mt {
+cudaError_t encode_matrix_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_cols,
+                              bool fp32) {
+  return make_tmap_strided(map, base, rows, cols, row_bytes, box_rows, box_cols, fp32);
+}
+}  // namespace mt

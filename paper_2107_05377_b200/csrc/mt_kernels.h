@@ -442,4 +442,104 @@ struct DropoutParams {
 };
 cudaError_t launch_dropout(const DropoutParams& p, bool x_f32, bool y_f32, int sm_count, cudaStream_t stream);
 
+// Tensor map of a row-major matrix [rows, cols], row_bytes from one row to the next (a multiple of 16), in boxes of box_rows x
+// box_cols whose rows are 128 bytes, with the 128-byte swizzle.
+cudaError_t encode_matrix_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_cols,
+                              bool fp32);
+
+// Softmax cross entropy over the vocabulary, and its gradient.  What a call is given:
+struct VocabLossCall {
+  const bf16* x;
+  const bf16* w;
+  const bf16* bias;            // or null
+  const int32_t* labels;       // outside [0, vocab): no loss, no gradient
+  int64_t x_stride, w_stride;
+  int32_t rows, vocab, hidden;
+  uint32_t* status;
+  void* workspace;
+  float* loss;                 // forward
+  float* lse_out;
+  const float* lse;            // backward
+  const float* grad_loss;      // or null: ones
+  bf16* dx;                    // each may be null
+  bf16* dw;
+  float* db;
+  int64_t dx_stride, dw_stride;
+  int32_t accumulate;          // (into dw and db)
+};
+size_t vocab_loss_workspace(int rows, int vocab, int hidden);
+size_t vocab_loss_grad_workspace(int rows, int vocab, int hidden);
+cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t stream);
+cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStream_t stream);
+
+// The products.  Index 1 of the maps of x: the rows with a label, gathered.  Boxes of 128 x 64 (block_n / 2 x 64) for operands along K,
+// 64 x 64 for operands whose rows run along K, 32 rows x 128 bytes for results.
+struct VocabLossParams {
+  CUtensorMap x_k[2], w_k, x_mn[2], w_mn, g_k, g_mn, g_out, dx_out, dw_out;
+  const bf16* bias;
+  const int32_t* labels;       // of the rows in use
+  const int32_t* count;        // rows in use (or null: rows)
+  const float* row_lse;
+  const float* row_weight;
+  float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
+  float2* parts;
+  float* bias_parts;           // backward: sums of g over 32 rows each, [block][bias_pitch]; or null
+  bf16* dw;
+  int64_t dw_stride;
+  uint32_t* counter;           // next tile to hand out
+  uint32_t* status;
+  int32_t rows, vocab, hidden, block_n, block_h;
+  int32_t col0, cols;          // columns of the vocabulary whose logits are taken
+  int32_t prev_col0, prev_cols;   // columns whose g is taken into the products (0: none)
+  int32_t g_row0, prev_g_row0; // first row of their buffers of g
+  int32_t row_pitch;           // rows in whole tiles
+  int32_t ranges;              // of the vocabulary, for dx
+  int32_t prev_first;          // dx is stored, not added to
+  int32_t part_pitch, bias_pitch;
+  int32_t want_x, want_w, accumulate;
+};
+struct VocabRowsParams {
+  const int32_t* labels;
+  const bf16* x;
+  const float* lse;
+  const float* grad_loss;
+  int64_t x_stride;
+  int32_t rows, vocab, hidden, rows_per_cta, n_counters;
+  int32_t* count;
+  uint32_t* counters;          // set to zero
+  int32_t* row_of;             // caller's row of a row in use
+  int32_t* place_of;           // the other way round (-1: none), or null
+  int32_t* row_label;
+  float* row_lse;              // or null
+  float* row_weight;           // or null
+  bf16* gathered;
+  float* loss_out;             // forward: zeros for rows without a label
+  float* lse_out;
+  uint32_t* status;
+};
+struct VocabJoinParams {
+  const int32_t* labels;
+  const int32_t* count;
+  const int32_t* row_of;
+  const float2* parts;
+  const float* label_logit;
+  float* loss;
+  float* lse;
+  int32_t rows, vocab, part_pitch, n_parts;
+  uint32_t* status;
+};
+struct VocabDxParams {
+  const float* sums;           // [ranges][row_pitch][hidden]
+  const int32_t* place_of;
+  bf16* dx;
+  int64_t dx_stride, row_pitch;
+  int32_t rows, hidden, ranges;
+};
+struct VocabBiasParams {
+  const float* parts;
+  const int32_t* count;
+  float* out;
+  int32_t rows, cols, pitch, accumulate;
+};
+
 }  // namespace mt

@@ -1,0 +1,984 @@
+// Softmax cross entropy over a large vocabulary without keeping the logits, and its gradient.
+//
+//   z = x W^T + b                                   x [rows, hidden], W [vocab, hidden], bf16; sums in fp32
+//   lse = log sum_v exp z_v,  loss = lse - z_label
+//   g = dloss (exp(z - lse) - onehot(label))        rounded to bf16, the operand of the two products below
+//   dx = g W,  dW = g^T x,  db = sum over rows of g (from g before rounding)
+//
+// The forward pass is one product whose epilogue keeps, for every row and tile of columns, the largest logit and the sum of
+// exponentials relative to it; a second kernel puts a row's tiles together.  The backward pass makes the logits again, a piece of the
+// vocabulary at a time, and keeps g of two pieces at most: launch j computes g of piece j and, among the same tiles, the two products
+// of piece j - 1, so that the tiles of all three fill the machine together and a piece costs one launch.
+//
+// All products are tiles of 256 x 256 of CTA pairs (tcgen05 cta_group::2, fp32 accumulators in tensor memory, two of them so that the
+// epilogue of a tile overlaps the next one's products):
+//   kind 0   z or g   M = rows, N = vocab,  K = hidden   both operands along K
+//   kind 1   dx       M = rows, N = hidden, K = vocab    g along K, W with its rows along K (MN-major)
+//   kind 2   dW       M = vocab, N = hidden, K = rows    g and x with their rows along K
+// so neither g nor any input is ever transposed in memory.  Rows without a label take no part: where there are some, the rows that have
+// one are gathered first (their places stay on the device; the grids are sized for all rows and bound their tiles by the count).
+//
+// dx is a sum over all pieces: kept in fp32 in the workspace, added to by TMA reductions (one tile per element and launch, so the
+// order is that of the launches), where a launch has few tiles of it in several ranges of the vocabulary with a place each; a last
+// kernel adds the ranges in order and rounds once.
+//
+// What bounds it: the tensor cores from some hundred rows on, below that the bytes of W (read twice) and dW.
+
+#include <cstring>
+
+#include "cluster_ptx.cuh"
+
+namespace mt {
+namespace {
+
+constexpr int kTile = 256;                 // rows and (at most) columns of a pair's tile
+constexpr int kHalf = 128;                 // rows of a CTA
+constexpr int kStageA = kHalf * 128;       // bytes: 128 rows of 64 elements, or two boxes of 64 x 64
+constexpr int kStageB = kHalf * 128;
+constexpr int kEpilogueWarps = 8;
+constexpr int kThreads = 32 * (2 + kEpilogueWarps);
+constexpr int kStaging = 4096;             // of an epilogue warp: 32 rows of 128 bytes
+constexpr int kBook = 1024;
+constexpr int kSlots = 4;                  // tiles announced ahead
+constexpr uint32_t kTmemCols = 512;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kFloor = -1e30f;           // below every logit that counts; finite, so that -inf minus it is no NaN
+
+__host__ __device__ constexpr int stages(bool grad) { return grad ? 6 : 7; }
+__host__ __device__ constexpr int smem_bytes(bool grad) {
+  return stages(grad) * (kStageA + kStageB) + (grad ? kEpilogueWarps * kStaging : 0) + kBook + 1024;
+}
+
+// Shared-memory descriptor of a tile whose 128-byte rows (64 elements of M or N, 128-byte swizzle) run along K: eight of them make an
+// atom, the next eight along K follow 1024 bytes on, the next 64 elements of M or N 8192 bytes on (boxes of 64 rows).
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t smem_addr) {
+  uint64_t d = static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(8192 >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+constexpr uint32_t kAlongMnA = 1u << 15, kAlongMnB = 1u << 16;   // instruction descriptor: the operand's rows run along K
+
+// Shared -> global addition of an fp32 tile; what lies outside the tensor is clipped.
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void st_cluster_u32(uint32_t cluster_addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+
+// The tiles of a launch, in the order in which they are handed out: long ones first.
+struct Work {
+  int row_tiles;               // 256 rows each
+  int n0, n1, n2;              // tiles of each kind
+  int k0, k1, k2;              // their k-blocks (k1: of one range of the vocabulary)
+  int row_k;                   // k-blocks that cover the rows
+  bool first1;                 // kind 1 before kind 2
+  int hidden_tiles;
+};
+struct Tile {
+  int kind, m, n, range, k_blocks, k_begin;
+};
+
+template <bool GRAD>
+__device__ __forceinline__ Work make_work(const VocabLossParams& p, int rows) {
+  Work w;
+  w.row_tiles = (rows + kTile - 1) / kTile;
+  w.n0 = w.row_tiles * ((p.cols + p.block_n - 1) / p.block_n);
+  w.k0 = (p.hidden + 63) / 64;
+  w.n1 = w.n2 = w.k1 = w.k2 = 0;
+  w.row_k = (rows + 63) / 64;
+  w.first1 = false;
+  w.hidden_tiles = 1;
+  if (GRAD) {
+    w.hidden_tiles = (p.hidden + p.block_h - 1) / p.block_h;
+    if (p.prev_cols > 0) {
+      if (p.want_x) w.n1 = w.row_tiles * w.hidden_tiles * p.ranges;
+      if (p.want_w) w.n2 = (p.prev_cols + kTile - 1) / kTile * w.hidden_tiles;
+      w.k1 = ((p.prev_cols + 63) / 64 + p.ranges - 1) / p.ranges;
+      w.k2 = w.row_k;
+      w.first1 = w.k1 > w.k2;
+    }
+  }
+  return w;
+}
+template <bool GRAD>
+__device__ __forceinline__ Tile find_tile(const VocabLossParams& p, const Work& w, int i) {
+  Tile t;
+  t.range = 0;
+  t.k_begin = 0;
+  if (GRAD && i < w.n1 + w.n2) {
+    const bool is1 = w.first1 ? i < w.n1 : i >= w.n2;
+    if (is1) {
+      if (!w.first1) i -= w.n2;
+      t.kind = 1;
+      t.m = i % w.row_tiles;
+      i /= w.row_tiles;
+      t.n = i % w.hidden_tiles;
+      t.range = i / w.hidden_tiles;
+      t.k_begin = t.range * w.k1;
+      const int all = (p.prev_cols + 63) / 64;
+      t.k_blocks = all - t.k_begin < w.k1 ? (all > t.k_begin ? all - t.k_begin : 0) : w.k1;
+    } else {
+      if (w.first1) i -= w.n1;
+      t.kind = 2;
+      const int m_tiles = w.n2 / w.hidden_tiles;
+      t.m = i % m_tiles;
+      t.n = i / m_tiles;
+      t.k_blocks = w.k2;
+    }
+    return t;
+  }
+  i -= w.n1 + w.n2;
+  t.kind = 0;
+  t.m = i % w.row_tiles;
+  t.n = i / w.row_tiles;
+  t.k_blocks = w.k0;
+  return t;
+}
+
+// Bias of 32 columns from `col` on (0 where there is none).
+__device__ __forceinline__ void add_bias(const bf16* bias, int col, int vocab, float (&z)[32]) {
+  if (bias == nullptr) return;
+  if (col + 32 <= vocab) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint4 b = __ldg(reinterpret_cast<const uint4*>(bias + col) + q);
+      const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        z[q * 8 + 2 * j] += bf16_lo(w[j]);
+        z[q * 8 + 2 * j + 1] += bf16_hi(w[j]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) if (col + j < vocab) z[j] += __bfloat162float(bias[col + j]);
+  }
+}
+
+// Sums over the 32 rows of a warp of 32 columns each, column `lane` in the result: halves of the columns are exchanged for halves of the
+// rows five times over (31 additions per lane instead of 160).
+__device__ __forceinline__ float column_sums(float (&c)[32], int lane) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool upper = (lane & o) != 0;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float give = upper ? c[i] : c[i + o];
+      const float keep = upper ? c[i + o] : c[i];
+      c[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  return c[0];
+}
+
+template <bool GRAD>
+__global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
+  constexpr int STAGES = stages(GRAD);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sA = smem_u32(smem);
+  const uint32_t sB = sA + STAGES * kStageA;
+  const uint32_t sStage = sB + STAGES * kStageB;
+  uint8_t* book = smem + STAGES * (kStageA + kStageB) + (GRAD ? kEpilogueWarps * kStaging : 0);
+  const uint32_t bar_full = smem_u32(book);
+  const uint32_t bar_empty = bar_full + 8 * STAGES;
+  const uint32_t bar_acc_full = bar_empty + 8 * STAGES;
+  const uint32_t bar_acc_empty = bar_acc_full + 16;
+  const uint32_t bar_slot_full = bar_acc_empty + 16;
+  const uint32_t bar_slot_empty = bar_slot_full + 8 * kSlots;      // (of rank 0)
+  volatile uint32_t* slot_tile = reinterpret_cast<volatile uint32_t*>(book + 8 * (2 * STAGES + 4 + 2 * kSlots));
+  uint32_t* tmem_slot = const_cast<uint32_t*>(slot_tile) + kSlots;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_cta_rank();
+  const int worker = static_cast<int>(blockIdx.x >> 1);
+  const int n_workers = static_cast<int>(gridDim.x >> 1);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(bar_acc_full + 8 * a, 1);
+      mbar_init(bar_acc_empty + 8 * a, 2 * kEpilogueWarps);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(bar_slot_full + 8 * s, 1);
+      mbar_init(bar_slot_empty + 8 * s, 2 * kEpilogueWarps + 2);   // all epilogue warps, the MMA warp, rank 1's producer
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), kTmemCols);
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t bar_full_count = map_to_cta(bar_full, 0);
+  const uint32_t bar_slot_empty_0 = map_to_cta(bar_slot_empty, 0);
+  if (warp == 0 && lane == 0) {
+    prefetch_tensormap(&p.x_k[0]);
+    prefetch_tensormap(&p.w_k);
+  }
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int rows = p.count != nullptr ? min(p.rows, *reinterpret_cast<const volatile int*>(p.count)) : p.rows;
+  const int gathered = rows == p.rows ? 0 : 1;      // which x: the caller's, or the rows with a label
+  const Work work = make_work<GRAD>(p, rows);
+  const int total = work.n0 + work.n1 + work.n2;
+
+  // Tiles.  Forward: worker, worker + n_workers, ... (all tiles cost the same).  Backward: the next of the list, whoever is free first;
+  // rank 0's producer takes them from a counter in memory and announces them to all roles of both CTAs.  (Which pair computes a tile
+  // has no influence on it.)
+  int slot = 0;
+  uint32_t slot_phase = 0;
+  // the roles other than rank 0's producer: the next tile, or -1 at the end and when the CTA is giving up
+  auto next_announced = [&]() -> int {
+    if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_slot_full + 8 * slot, slot_phase, abort_flag))) return -1;
+    const int i = static_cast<int>(slot_tile[slot]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive_cluster(bar_slot_empty_0 + 8 * slot);
+    if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
+    return i < total ? i : -1;
+  };
+
+  if (warp == 0) {
+    // ------------------------------ TMA producer ------------------------------
+    const bool leader = elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    long long issued = 0;
+    bool ok = true;
+    int taken = worker;                            // (static: the tile; dynamic, rank 0: asked for one tile ahead)
+    for (bool begun = false; ok; begun = true) {
+      int i;
+      if (!GRAD) {
+        if (begun) taken += n_workers;
+        i = taken < total ? taken : -1;
+      } else if (rank != 0) {
+        i = next_announced();
+      } else {
+        if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) { ok = false; break; }
+        i = __shfl_sync(0xffffffffu, taken, 0);
+        if (lane == 0) {
+          for (uint32_t r = 0; r < 2; ++r) {
+            st_cluster_u32(map_to_cta(smem_u32(const_cast<uint32_t*>(slot_tile) + slot), r), static_cast<uint32_t>(i));
+            mbar_arrive_cluster(map_to_cta(bar_slot_full + 8 * slot, r));
+          }
+        }
+        if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
+        if (i >= total) i = -1;
+        else if (lane == 0) taken = n_workers + static_cast<int>(atomicAdd(p.counter, 1u));   // the one after this
+      }
+      if (i < 0) break;
+      const Tile t = find_tile<GRAD>(p, work, i);
+      const int half_n = (t.kind == 0 ? p.block_n : p.block_h) / 2;
+      const uint32_t bytes = 2 * (kStageA + half_n * 128);
+      const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf;
+      const int n0 = t.n * (2 * half_n) + static_cast<int>(rank) * half_n;
+      for (int kb = 0; kb < t.k_blocks; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag))) { ok = false; break; }
+        if (leader) {
+          const uint32_t a = sA + stage * kStageA, b = sB + stage * kStageB, bar = bar_full_count + 8 * stage;
+          const int k = (t.k_begin + kb) * 64;
+          if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, bytes);
+          if (!GRAD || t.kind == 0) {
+            tma_load_2d_pair(a, &p.x_k[gathered], k, m0, bar);
+            tma_load_2d_pair(b, &p.w_k, k, p.col0 + n0, bar);
+          } else if (t.kind == 1) {
+            tma_load_2d_pair(a, &p.g_k, k, p.prev_g_row0 + m0, bar);
+            tma_load_2d_pair(b, &p.w_mn, n0, p.prev_col0 + k, bar);
+            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, p.prev_col0 + k, bar);
+          } else {
+            tma_load_2d_pair(a, &p.g_mn, m0, p.prev_g_row0 + k, bar);
+            tma_load_2d_pair(a + 8192, &p.g_mn, m0 + 64, p.prev_g_row0 + k, bar);
+            tma_load_2d_pair(b, &p.x_mn[gathered], n0, k, bar);
+            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, k, bar);
+          }
+        }
+        ++issued;
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok && rank == 0 && leader) {
+      // giving up: what is still in flight gets the same limit to land
+      const int pending = issued < STAGES ? static_cast<int>(issued) : STAGES;
+      for (int i = 0; i < pending; ++i) {
+        if (stage == 0) { stage = STAGES; phase ^= 1u; }
+        --stage;
+        mbar_drain(bar_full + 8 * stage, phase);
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------ MMA issuer --------------------------------
+    const bool leader = elect_one();
+    if (rank == 0) {
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      int taken = worker;
+      for (bool begun = false; ok; begun = true) {
+        int i;
+        if (GRAD) {
+          i = next_announced();
+        } else {
+          if (begun) taken += n_workers;
+          i = taken < total ? taken : -1;
+        }
+        if (i < 0) break;
+        const Tile t = find_tile<GRAD>(p, work, i);
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) break;
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kTile);
+        const bool mn_a = GRAD && t.kind == 2, mn_b = GRAD && t.kind != 0;
+        const uint32_t idesc = umma_idesc_bf16(kTile, t.kind == 0 ? p.block_n : p.block_h) | (mn_a ? kAlongMnA : 0u) | (mn_b ? kAlongMnB : 0u);
+        // 16 elements of K on: 32 bytes inside a row, or 16 rows
+        const uint64_t step_a = mn_a ? 2048 >> 4 : 2, step_b = mn_b ? 2048 >> 4 : 2;
+        for (int kb = 0; kb < t.k_blocks; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
+          tc_fence_after();
+          if (leader) {
+            const uint64_t da = mn_a ? smem_desc_mn(sA + stage * kStageA) : smem_desc_sw128(sA + stage * kStageA);
+            const uint64_t db = mn_b ? smem_desc_mn(sB + stage * kStageB) : smem_desc_sw128(sB + stage * kStageB);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) umma_bf16_pair(d_tmem, da + step_a * k, db + step_b * k, idesc, (kb | k) != 0 ? 1u : 0u);
+            umma_commit_pair(bar_empty + 8 * stage);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        if (leader) umma_commit_pair(bar_acc_full + 8 * acc);
+        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      }
+    }
+  } else {
+    // ------------------------------ epilogue ----------------------------------
+    const int e = warp - 2;
+    const int quarter = warp & 3;
+    const int group = e >> 2;                           // of the two that share the chunks of columns
+    const uint32_t my_stage = sStage + static_cast<uint32_t>(e * kStaging);
+    uint8_t* my_stage_ptr = smem + STAGES * (kStageA + kStageB) + e * kStaging;
+    const uint32_t bar_acc_empty_0 = map_to_cta(bar_acc_empty, 0);
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    int taken = worker;
+    for (bool begun = false;; begun = true) {
+      int i;
+      if (GRAD) {
+        i = next_announced();
+      } else {
+        if (begun) taken += n_workers;
+        i = taken < total ? taken : -1;
+      }
+      if (i < 0) break;
+      const Tile t = find_tile<GRAD>(p, work, i);
+      const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32;   // of this warp
+      const int row = m0 + lane;
+      const bool row_counts = row < rows;
+      int label = -1;
+      float minus_lse2 = 0.f, weight = 0.f;
+      if (t.kind == 0 && row_counts) {
+        label = p.labels[row];
+        if (GRAD) {
+          minus_lse2 = -p.row_lse[row] * kLog2e;
+          weight = p.row_weight[row];
+        }
+      }
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * acc, acc_phase, abort_flag))) break;
+      tc_fence_after();
+      const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc * kTile);
+      if (!GRAD) {
+        float top2 = kFloor, sum = 0.f;                 // largest logit times log2 e, sum of 2^(z log2 e - top2)
+        const int n0 = t.n * p.block_n;
+#pragma unroll 1
+        for (int c = group * 32; c < p.block_n; c += 64) {
+          const int col = n0 + c;
+          if (col >= p.vocab) break;
+          uint32_t v[32];
+          tmem_ld_32x32(taddr0 + c, v);
+          tmem_ld_wait();
+          float z[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
+          add_bias(p.bias, col, p.vocab, z);
+          if (col + 32 > p.vocab) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) if (col + j >= p.vocab) z[j] = -INFINITY;
+          }
+          const int at = label - col;
+          if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+            float mine = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) if (j == at) mine = z[j];
+            if (at >= 0 && at < 32) p.label_logit[row] = mine;
+          }
+          float m = z[0];
+#pragma unroll
+          for (int j = 1; j < 32; ++j) m = fmaxf(m, z[j]);
+          const float next2 = fmaxf(top2, m * kLog2e);
+          sum *= ex2_approx(top2 - next2);
+          top2 = next2;
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[j & 3] += ex2_approx(fmaf(z[j], kLog2e, -top2));
+          sum += (s[0] + s[1]) + (s[2] + s[3]);
+        }
+        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + 2 * t.n + group] = make_float2(top2, sum);
+      } else if (t.kind == 0) {
+        const int n0 = t.n * p.block_n;                 // in the piece
+        const bool whole = __all_sync(0xffffffffu, row_counts);
+#pragma unroll 1
+        for (int c = group * 64; c < p.block_n; c += 128) {
+          if (n0 + c >= p.cols) break;
+          // the store that last read this buffer must be done with it
+          if (lane == 0) tma_store_wait_read<0>();
+          __syncwarp();
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int local = n0 + c + half * 32;
+            const int col = p.col0 + local;
+            uint32_t v[32];
+            tmem_ld_32x32(taddr0 + c + half * 32, v);
+            tmem_ld_wait();
+            float g[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(v[j]);
+            add_bias(p.bias, col, p.vocab, g);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, minus_lse2));
+            const int at = label - col;
+            if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) if (j == at) g[j] -= 1.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] *= weight;
+            if (!whole) {                               // (behind the last row lies anything)
+#pragma unroll
+              for (int j = 0; j < 32; ++j) g[j] = row_counts ? g[j] : 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<uint4*>(my_stage_ptr + staging_off(lane, half * 4 + q)) =
+                  make_uint4(pack_bf16(g[q * 8], g[q * 8 + 1]), pack_bf16(g[q * 8 + 2], g[q * 8 + 3]), pack_bf16(g[q * 8 + 4], g[q * 8 + 5]),
+                             pack_bf16(g[q * 8 + 6], g[q * 8 + 7]));
+            if (p.bias_parts != nullptr && m0 < rows) {
+              const float s = column_sums(g, lane);
+              if (local + lane < p.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + local + lane] = s;
+            }
+          }
+          fence_async_shared();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(&p.g_out, my_stage, n0 + c, p.g_row0 + m0);
+            tma_store_commit();
+          }
+        }
+      } else if (t.kind == 1) {
+        const int n0 = t.n * p.block_h;
+#pragma unroll 1
+        for (int c = group * 32; c < p.block_h; c += 64) {
+          if (n0 + c >= p.hidden || m0 >= rows) break;
+          if (lane == 0) tma_store_wait_read<0>();
+          __syncwarp();
+          uint32_t v[32];
+          if (t.k_blocks > 0) {
+            tmem_ld_32x32(taddr0 + c, v);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = 0u;
+          }
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            *reinterpret_cast<uint4*>(my_stage_ptr + staging_off(lane, q)) = make_uint4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
+          fence_async_shared();
+          __syncwarp();
+          if (lane == 0) {
+            if (p.prev_first) tma_store_2d(&p.dx_out, my_stage, n0 + c, t.range * p.row_pitch + m0);
+            else tma_add_2d(&p.dx_out, my_stage, n0 + c, t.range * p.row_pitch + m0);
+            tma_store_commit();
+          }
+        }
+      } else {
+        const int n0 = t.n * p.block_h;
+        const int word = p.prev_col0 + row;             // row of dW
+#pragma unroll 1
+        for (int c = group * 64; c < p.block_h; c += 128) {
+          if (n0 + c >= p.hidden || p.prev_col0 + m0 >= p.vocab) break;
+          if (lane == 0) tma_store_wait_read<0>();
+          __syncwarp();
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int col = n0 + c + half * 32;
+            uint32_t v[32];
+            if (t.k_blocks > 0) {
+              tmem_ld_32x32(taddr0 + c + half * 32, v);
+              tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = 0u;
+            }
+            if (p.accumulate) {
+              const bf16* old = p.dw + static_cast<int64_t>(word) * p.dw_stride + col;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {             // (hidden is a multiple of eight)
+                if (word >= p.vocab || col + q * 8 >= p.hidden) continue;
+                const uint4 b = *reinterpret_cast<const uint4*>(old + q * 8);
+                const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  v[q * 8 + 2 * j] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j]) + bf16_lo(w[j]));
+                  v[q * 8 + 2 * j + 1] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j + 1]) + bf16_hi(w[j]));
+                }
+              }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              uint32_t o[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[j] = pack_bf16(__uint_as_float(v[q * 8 + 2 * j]), __uint_as_float(v[q * 8 + 2 * j + 1]));
+              *reinterpret_cast<uint4*>(my_stage_ptr + staging_off(lane, half * 4 + q)) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+          }
+          fence_async_shared();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(&p.dw_out, my_stage, n0 + c, p.prev_col0 + m0);
+            tma_store_commit();
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(bar_acc_empty_0 + 8 * acc);
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    }
+    if (lane == 0) tma_store_wait_read<0>();
+    __syncwarp();
+  }
+
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();
+  if (threadIdx.x == 0 && *abort_flag && p.status != nullptr) atomicOr(p.status, kFlagWaitTimeout);
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, kTmemCols);
+  }
+}
+
+// ---- rows with a label ---------------------------------------------------------------------------
+
+constexpr int kRowsThreads = 256;
+
+// A CTA per `rows_per_cta` rows counts the labels before them and all of them (a few KB that stay in L2), and gives every row with a
+// label its place.  Unless all rows have one, their hidden states are gathered, with zeros up to the next k-block of the products that
+// sum over rows.
+__global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_constant__ VocabRowsParams p) {
+  __shared__ int s_before, s_all;
+  __shared__ int s_warp[kRowsThreads / 32];
+  __shared__ int s_place[kRowsThreads];
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int first = blockIdx.x * p.rows_per_cta;
+  const int last = min(first + p.rows_per_cta, p.rows);
+  auto has_label = [&](int r) { const int l = p.labels[r]; return l >= 0 && l < p.vocab; };
+  if (tid == 0) s_before = s_all = 0;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll 4
+  for (int r = tid; r < p.rows; r += kRowsThreads) {
+    const int has = has_label(r) ? 1 : 0;
+    all += has;
+    if (r < first) before += has;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+    all += __shfl_xor_sync(0xffffffffu, all, o);
+  }
+  if (lane == 0) {
+    atomicAdd(&s_before, before);          // (whole numbers: any order)
+    atomicAdd(&s_all, all);
+  }
+  __syncthreads();
+  all = s_all;
+  if (blockIdx.x == 0) {
+    if (tid == 0) *p.count = all;
+    for (int i = tid; i < p.n_counters; i += kRowsThreads) p.counters[i] = 0;
+  }
+  const int vectors = p.hidden / 8;
+  for (int r0 = first; r0 < last; r0 += kRowsThreads) {
+    // places of up to 256 rows, then their copies, a warp per row
+    const int r = r0 + tid;
+    const bool has = r < last && has_label(r);
+    const uint32_t mask = __ballot_sync(0xffffffffu, has);
+    if (lane == 0) s_warp[warp] = __popc(mask);
+    __syncthreads();
+    int place = s_before + __popc(mask & ((1u << lane) - 1));
+    for (int w = 0; w < warp; ++w) place += s_warp[w];
+    s_place[tid] = has ? place : -1;
+    if (r < last) {
+      if (p.labels[r] >= p.vocab && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
+      if (p.place_of != nullptr) p.place_of[r] = has ? place : -1;
+      if (has) {
+        p.row_of[place] = r;
+        p.row_label[place] = p.labels[r];
+        if (p.row_lse != nullptr) p.row_lse[place] = p.lse[r];
+        if (p.row_weight != nullptr) p.row_weight[place] = p.grad_loss != nullptr ? p.grad_loss[r] : 1.f;
+      } else if (p.loss_out != nullptr) {
+        p.loss_out[r] = 0.f;
+        p.lse_out[r] = 0.f;
+      }
+    }
+    __syncthreads();
+    if (all != p.rows) {
+      const int end = min(kRowsThreads, last - r0);
+      for (int i = warp; i < end; i += kRowsThreads / 32) {
+        const int to = s_place[i];
+        if (to < 0) continue;
+        const uint4* src = reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(r0 + i) * p.x_stride);
+        uint4* dst = reinterpret_cast<uint4*>(p.gathered + static_cast<int64_t>(to) * p.hidden);
+#pragma unroll 4
+        for (int c = lane; c < vectors; c += 32) dst[c] = __ldg(src + c);
+      }
+    }
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 0; w < kRowsThreads / 32; ++w) s_before += s_warp[w];
+    }
+    __syncthreads();
+  }
+  if (all != p.rows && blockIdx.x == 0) {
+    const int64_t from = static_cast<int64_t>(all) * vectors, to = static_cast<int64_t>((all + 63) / 64 * 64) * vectors;
+    for (int64_t i = from + tid; i < to; i += kRowsThreads) reinterpret_cast<uint4*>(p.gathered)[i] = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ---- a row's tiles put together ------------------------------------------------------------------
+
+constexpr int kJoinThreads = 128;
+
+// A warp per row: log-sum-exp and loss from (largest logit, sum) of every half tile.
+__global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __grid_constant__ VocabJoinParams p) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int rows = p.count != nullptr ? min(p.rows, *reinterpret_cast<const volatile int*>(p.count)) : p.rows;
+  const int step = gridDim.x * (kJoinThreads / 32);
+  for (int row = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); row < rows; row += step) {
+    const int label = p.labels[row];
+    const int to = p.row_of != nullptr ? p.row_of[row] : row;
+    if (label < 0 || label >= p.vocab) {             // (only where the rows were not gathered)
+      if (lane == 0) {
+        if (label >= p.vocab && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
+        p.loss[to] = 0.f;
+        p.lse[to] = 0.f;
+      }
+      continue;
+    }
+    const float2* parts = p.parts + static_cast<int64_t>(row) * p.part_pitch;
+    float top = kFloor;
+    for (int i = lane; i < p.n_parts; i += 32) top = fmaxf(top, parts[i].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float sum = 0.f;
+    for (int i = lane; i < p.n_parts; i += 32) {
+      const float2 part = parts[i];
+      sum += part.y * exp2f(part.x - top);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) {
+      const float log_sum = logf(sum);
+      p.lse[to] = fmaf(top, kLn2, log_sum);
+      p.loss[to] = fmaf(top, kLn2, -p.label_logit[row]) + log_sum;
+    }
+  }
+}
+
+// dx: the ranges of a row added up in order, rounded once, to the row's place; zeros for rows without a label.  A warp per row.
+__global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_constant__ VocabDxParams p) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int step = gridDim.x * (kJoinThreads / 32);
+  for (int row = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); row < p.rows; row += step) {
+    const int place = p.place_of[row];
+    bf16* out = p.dx + static_cast<int64_t>(row) * p.dx_stride;
+    for (int c = lane * 8; c < p.hidden; c += 256) {
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+      if (place >= 0) {
+        const float* src = p.sums + static_cast<int64_t>(place) * p.hidden + c;
+#pragma unroll 4
+        for (int s = 0; s < p.ranges; ++s) {
+          const float4* f = reinterpret_cast<const float4*>(src + static_cast<int64_t>(s) * p.row_pitch * p.hidden);
+          const float4 u = f[0], w = f[1];
+          a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
+          b.x += w.x; b.y += w.y; b.z += w.z; b.w += w.w;
+        }
+      }
+      *reinterpret_cast<uint4*>(out + c) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+    }
+  }
+}
+
+// db of a piece: the sums of all blocks of 32 rows, in order.  A CTA per 32 columns; every warp takes each eighth block.
+__global__ void __launch_bounds__(256) vocab_bias_kernel(const __grid_constant__ VocabBiasParams p) {
+  __shared__ float s_sum[8][32];
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rows = min(p.rows, *reinterpret_cast<const volatile int*>(p.count));
+  const int blocks = (rows + 31) / 32;
+  const int col = blockIdx.x * 32 + lane;
+  float sum = 0.f;
+  if (col < p.cols) {
+#pragma unroll 8
+    for (int b = warp; b < blocks; b += 8) sum += p.parts[static_cast<int64_t>(b) * p.pitch + col];
+  }
+  s_sum[warp][lane] = sum;
+  __syncthreads();
+  if (warp != 0 || col >= p.cols) return;
+  for (int w = 1; w < 8; ++w) sum += s_sum[w][lane];
+  p.out[col] = p.accumulate ? p.out[col] + sum : sum;
+}
+
+template <bool GRAD>
+cudaError_t launch_pairs(const VocabLossParams& p, int tiles, int sm_count, cudaStream_t stream) {
+  auto kernel = vocab_loss_pair_tcgen05<GRAD>;
+  static PerDeviceOnce once;
+  cudaError_t err = per_device_once(once, [&](int) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes(GRAD));
+  });
+  if (err != cudaSuccess) return err;
+  const int most = sm_count / 2 > 0 ? sm_count / 2 : 1;
+  const int workers = tiles < most ? (tiles > 0 ? tiles : 1) : most;
+  return launch_kernel(kernel, dim3(2 * workers), dim3(kThreads), smem_bytes(GRAD), stream, p, 2u);
+}
+
+int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
+size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// ---- plans -----------------------------------------------------------------------------------------
+
+constexpr int kGatherRows = kTile;       // up to one tile of rows costs the same however few of them count
+constexpr int64_t kPieceElements = 32 << 20;   // of g of one piece: 64 MB
+constexpr int kMinPiece = 2048;
+constexpr int kMaxRanges = 32;
+
+struct ForwardPlan {
+  int block_n, tiles_n, part_pitch;
+  int64_t row_pitch;                     // rows in whole tiles
+  bool gather;
+  size_t count, row_of, row_label, label_logit, parts, gathered, bytes;
+};
+ForwardPlan forward_plan(int rows, int vocab, int hidden, int sm_count) {
+  ForwardPlan f;
+  f.row_pitch = static_cast<int64_t>(ceil_div(rows, kTile)) * kTile;
+  f.gather = rows > kGatherRows;
+  // Width of the tiles: the last round of pairs is as full as can be.  With many tiles the widest (fewest bytes staged per product);
+  // with one tile of rows the pairs' columns decide, e.g. 30522 of them on 74 pairs: two rounds of 224 instead of two of 256.
+  const int pairs = sm_count / 2 > 0 ? sm_count / 2 : 1;
+  const int m = static_cast<int>(f.row_pitch / kTile);
+  int64_t best = -1;
+  f.block_n = kTile;
+  for (int bn = kTile; bn >= kHalf; bn -= 32) {
+    const int64_t tiles = static_cast<int64_t>(m < 1 ? 1 : m) * ceil_div(vocab, bn);
+    const int64_t cost = (tiles + pairs - 1) / pairs * (bn + 16);
+    if (best < 0 || cost < best) { best = cost; f.block_n = bn; }
+  }
+  f.tiles_n = ceil_div(vocab, f.block_n);
+  f.part_pitch = 2 * f.tiles_n;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += whole_lines(bytes); return here; };
+  f.count = take(256);
+  f.row_of = take(f.row_pitch * 4);
+  f.row_label = take(f.row_pitch * 4);
+  f.label_logit = take(f.row_pitch * 4);
+  f.parts = take(static_cast<size_t>(f.row_pitch) * ceil_div(vocab, kHalf) * 2 * sizeof(float2));   // (for the narrowest tiles)
+  f.gathered = take(f.gather ? static_cast<size_t>(f.row_pitch) * hidden * 2 : 0);
+  f.bytes = at;
+  return f;
+}
+
+struct GradPlan {
+  int piece, pieces, buffers, block_h, ranges;
+  int64_t row_pitch;
+  size_t count, counters, row_of, row_label, row_lse, row_weight, place_of, gathered, g, dx, bias_parts, bytes;
+};
+GradPlan grad_plan(int rows, int vocab, int hidden) {
+  GradPlan f;
+  f.row_pitch = static_cast<int64_t>(ceil_div(rows, kTile)) * kTile;
+  const int m = static_cast<int>(f.row_pitch / kTile);
+  const int64_t all = static_cast<int64_t>(ceil_div(vocab, kTile)) * kTile;
+  int64_t piece = kPieceElements / (f.row_pitch > 0 ? f.row_pitch : 1) / kTile * kTile;
+  if (piece < kMinPiece) piece = kMinPiece;
+  f.pieces = ceil_div(all, piece);
+  f.piece = static_cast<int>(ceil_div(all / kTile, f.pieces)) * kTile;      // (pieces of the same size)
+  f.pieces = ceil_div(all, f.piece);
+  f.buffers = f.pieces > 1 ? 2 : 1;
+  f.block_h = hidden > kHalf ? kTile : kHalf;
+  // Ranges of the vocabulary that dx of a piece is summed over in: a tile of it should be no longer than half of what a pair has to do
+  // in the launch (a tile counts as at least six k-blocks: its epilogue).
+  const int h = ceil_div(hidden, f.block_h);
+  const int k1 = f.piece / 64, k2 = ceil_div(rows, 64), k0 = ceil_div(hidden, 64);
+  const int64_t all_k = static_cast<int64_t>(m) * h * k1 + static_cast<int64_t>(f.piece / kTile) * h * (k2 > 6 ? k2 : 6) +
+                        (f.pieces > 1 ? static_cast<int64_t>(m) * (f.piece / kTile) * (k0 > 6 ? k0 : 6) : 0);
+  int64_t longest = all_k / 74 / 2;
+  if (longest < 8) longest = 8;
+  f.ranges = ceil_div(k1, longest);
+  if (f.ranges > kMaxRanges) f.ranges = kMaxRanges;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += whole_lines(bytes); return here; };
+  f.count = take(256);
+  f.counters = take((static_cast<size_t>(f.pieces) + 1) * 4);
+  f.row_of = take(f.row_pitch * 4);
+  f.row_label = take(f.row_pitch * 4);
+  f.row_lse = take(f.row_pitch * 4);
+  f.row_weight = take(f.row_pitch * 4);
+  f.place_of = take(f.row_pitch * 4);
+  f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
+  f.g = take(static_cast<size_t>(f.buffers) * f.row_pitch * f.piece * 2);
+  f.dx = take(static_cast<size_t>(f.ranges) * f.row_pitch * hidden * 4);
+  f.bias_parts = take(static_cast<size_t>(f.row_pitch / 32) * f.piece * 4);
+  f.bytes = at;
+  return f;
+}
+
+void launch_rows_setup(VocabRowsParams* r, int* ctas) {
+  // at most 1024 CTAs, each of which reads all labels
+  r->rows_per_cta = ceil_div(r->rows, 1024) > 32 ? ceil_div(r->rows, 1024) : 32;
+  *ctas = ceil_div(r->rows, r->rows_per_cta);
+}
+template <typename T>
+T* at(void* base, size_t offset) { return reinterpret_cast<T*>(static_cast<uint8_t*>(base) + offset); }
+
+}  // namespace
+
+size_t vocab_loss_workspace(int rows, int vocab, int hidden) { return forward_plan(rows, vocab, hidden, 148).bytes; }
+size_t vocab_loss_grad_workspace(int rows, int vocab, int hidden) { return grad_plan(rows, vocab, hidden).bytes; }
+
+cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t stream) {
+  const ForwardPlan f = forward_plan(c.rows, c.vocab, c.hidden, sm_count);
+  void* ws = c.workspace;
+  cudaError_t e;
+  if (f.gather) {
+    VocabRowsParams r;
+    memset(&r, 0, sizeof(r));
+    r.labels = c.labels; r.x = c.x; r.x_stride = c.x_stride; r.rows = c.rows; r.vocab = c.vocab; r.hidden = c.hidden;
+    r.count = at<int32_t>(ws, f.count); r.row_of = at<int32_t>(ws, f.row_of); r.row_label = at<int32_t>(ws, f.row_label);
+    r.gathered = at<bf16>(ws, f.gathered); r.loss_out = c.loss; r.lse_out = c.lse_out; r.status = c.status;
+    int ctas = 0;
+    launch_rows_setup(&r, &ctas);
+    if ((e = launch_kernel(vocab_rows_kernel, dim3(ctas), dim3(kRowsThreads), 0, stream, r)) != cudaSuccess) return e;
+  }
+  VocabLossParams p;
+  memset(&p, 0, sizeof(p));
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.cols = c.vocab; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
+  p.labels = f.gather ? at<int32_t>(ws, f.row_label) : c.labels;
+  p.count = f.gather ? at<int32_t>(ws, f.count) : nullptr;
+  p.label_logit = at<float>(ws, f.label_logit); p.parts = at<float2>(ws, f.parts); p.part_pitch = f.part_pitch; p.status = c.status;
+  if ((e = encode_matrix_map(&p.x_k[0], c.x, c.rows, c.hidden, c.x_stride * 2, kHalf, 64, false)) != cudaSuccess) return e;
+  p.x_k[1] = p.x_k[0];
+  if (f.gather &&
+      (e = encode_matrix_map(&p.x_k[1], at<bf16>(ws, f.gathered), f.row_pitch, c.hidden, static_cast<int64_t>(c.hidden) * 2, kHalf, 64, false)) != cudaSuccess)
+    return e;
+  if ((e = encode_matrix_map(&p.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, f.block_n / 2, 64, false)) != cudaSuccess) return e;
+  if ((e = launch_pairs<false>(p, static_cast<int>(f.row_pitch / kTile) * f.tiles_n, sm_count, stream)) != cudaSuccess) return e;
+  VocabJoinParams j;
+  memset(&j, 0, sizeof(j));
+  j.labels = p.labels; j.count = p.count; j.row_of = f.gather ? at<int32_t>(ws, f.row_of) : nullptr; j.parts = p.parts;
+  j.part_pitch = f.part_pitch; j.n_parts = f.part_pitch; j.label_logit = p.label_logit; j.loss = c.loss; j.lse = c.lse_out;
+  j.rows = c.rows; j.vocab = c.vocab; j.status = c.status;
+  const int ctas = ceil_div(c.rows, kJoinThreads / 32);
+  return launch_kernel(vocab_loss_join_kernel, dim3(ctas < 16 * sm_count ? ctas : 16 * sm_count), dim3(kJoinThreads), 0, stream, j);
+}
+
+cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStream_t stream) {
+  const GradPlan f = grad_plan(c.rows, c.vocab, c.hidden);
+  void* ws = c.workspace;
+  cudaError_t e;
+  VocabRowsParams r;
+  memset(&r, 0, sizeof(r));
+  r.labels = c.labels; r.x = c.x; r.x_stride = c.x_stride; r.rows = c.rows; r.vocab = c.vocab; r.hidden = c.hidden;
+  r.count = at<int32_t>(ws, f.count); r.row_of = at<int32_t>(ws, f.row_of); r.row_label = at<int32_t>(ws, f.row_label);
+  r.row_lse = at<float>(ws, f.row_lse); r.row_weight = at<float>(ws, f.row_weight); r.place_of = at<int32_t>(ws, f.place_of);
+  r.lse = c.lse; r.grad_loss = c.grad_loss; r.gathered = at<bf16>(ws, f.gathered);
+  r.counters = at<uint32_t>(ws, f.counters); r.n_counters = f.pieces + 1; r.status = c.status;
+  int ctas = 0;
+  launch_rows_setup(&r, &ctas);
+  if ((e = launch_kernel(vocab_rows_kernel, dim3(ctas), dim3(kRowsThreads), 0, stream, r)) != cudaSuccess) return e;
+
+  VocabLossParams p;
+  memset(&p, 0, sizeof(p));
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias;
+  p.labels = r.row_label; p.count = r.count; p.row_lse = r.row_lse; p.row_weight = r.row_weight;
+  p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.status = c.status;
+  p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate;
+  p.dw = c.dw; p.dw_stride = c.dw_stride;
+  p.bias_parts = c.db != nullptr ? at<float>(ws, f.bias_parts) : nullptr; p.bias_pitch = f.piece;
+  bf16* gathered = at<bf16>(ws, f.gathered);
+  bf16* g = at<bf16>(ws, f.g);
+  const int64_t g_rows = f.buffers * f.row_pitch, g_stride = static_cast<int64_t>(f.piece) * 2, h_stride = static_cast<int64_t>(c.hidden) * 2;
+  if ((e = encode_matrix_map(&p.x_k[0], c.x, c.rows, c.hidden, c.x_stride * 2, kHalf, 64, false)) != cudaSuccess ||
+      (e = encode_matrix_map(&p.x_k[1], gathered, f.row_pitch, c.hidden, h_stride, kHalf, 64, false)) != cudaSuccess ||
+      (e = encode_matrix_map(&p.x_mn[0], c.x, c.rows, c.hidden, c.x_stride * 2, 64, 64, false)) != cudaSuccess ||
+      (e = encode_matrix_map(&p.x_mn[1], gathered, f.row_pitch, c.hidden, h_stride, 64, 64, false)) != cudaSuccess ||
+      (e = encode_matrix_map(&p.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, kHalf, 64, false)) != cudaSuccess ||
+      (e = encode_matrix_map(&p.w_mn, c.w, c.vocab, c.hidden, c.w_stride * 2, 64, 64, false)) != cudaSuccess ||
+      (e = encode_matrix_map(&p.dx_out, at<float>(ws, f.dx), f.ranges * f.row_pitch, c.hidden, static_cast<int64_t>(c.hidden) * 4, 32, 32, true)) != cudaSuccess)
+    return e;
+  if (c.dw != nullptr && (e = encode_matrix_map(&p.dw_out, c.dw, c.vocab, c.hidden, c.dw_stride * 2, 32, 64, false)) != cudaSuccess) return e;
+  const bool products = c.dx != nullptr || c.dw != nullptr;
+  const int row_tiles = static_cast<int>(f.row_pitch / kTile), hidden_tiles = ceil_div(c.hidden, f.block_h);
+  for (int j = 0; j <= f.pieces; ++j) {
+    if (j == f.pieces && !products) break;
+    p.col0 = j * f.piece;
+    p.cols = j < f.pieces ? (c.vocab - p.col0 < f.piece ? c.vocab - p.col0 : f.piece) : 0;
+    p.g_row0 = (j & (f.buffers - 1)) * static_cast<int>(f.row_pitch);
+    p.prev_col0 = (j - 1) * f.piece;
+    p.prev_cols = j > 0 ? (c.vocab - p.prev_col0 < f.piece ? c.vocab - p.prev_col0 : f.piece) : 0;
+    p.prev_g_row0 = j > 0 ? ((j - 1) & (f.buffers - 1)) * static_cast<int>(f.row_pitch) : 0;
+    p.prev_first = j == 1 ? 1 : 0;
+    p.counter = r.counters + j;
+    // (columns behind the piece's last one are neither stored nor read: the products over the vocabulary see zeros there)
+    if (p.cols > 0 && (e = encode_matrix_map(&p.g_out, g, g_rows, p.cols, g_stride, 32, 64, false)) != cudaSuccess) return e;
+    if (p.prev_cols > 0 && ((e = encode_matrix_map(&p.g_k, g, g_rows, p.prev_cols, g_stride, kHalf, 64, false)) != cudaSuccess ||
+                            (e = encode_matrix_map(&p.g_mn, g, g_rows, p.prev_cols, g_stride, 64, 64, false)) != cudaSuccess))
+      return e;
+    const int64_t tiles = static_cast<int64_t>(row_tiles) * ceil_div(p.cols, kTile) +
+                          (p.prev_cols > 0 ? static_cast<int64_t>(row_tiles) * hidden_tiles * f.ranges + static_cast<int64_t>(ceil_div(p.prev_cols, kTile)) * hidden_tiles : 0);
+    if ((e = launch_pairs<true>(p, static_cast<int>(tiles < (1 << 30) ? tiles : 1 << 30), sm_count, stream)) != cudaSuccess) return e;
+    if (c.db != nullptr && j < f.pieces) {
+      VocabBiasParams b;
+      memset(&b, 0, sizeof(b));
+      b.parts = p.bias_parts; b.pitch = f.piece; b.count = r.count; b.rows = c.rows; b.cols = p.cols; b.out = c.db + p.col0; b.accumulate = c.accumulate;
+      if ((e = launch_kernel(vocab_bias_kernel, dim3(ceil_div(p.cols, 32)), dim3(256), 0, stream, b)) != cudaSuccess) return e;
+    }
+  }
+  if (c.dx == nullptr) return cudaSuccess;
+  VocabDxParams d;
+  memset(&d, 0, sizeof(d));
+  d.sums = at<float>(ws, f.dx); d.place_of = r.place_of; d.dx = c.dx; d.dx_stride = c.dx_stride; d.rows = c.rows; d.hidden = c.hidden;
+  d.row_pitch = f.row_pitch; d.ranges = f.ranges;
+  const int dx_ctas = ceil_div(c.rows, kJoinThreads / 32);
+  return launch_kernel(vocab_dx_kernel, dim3(dx_ctas < 16 * sm_count ? dx_ctas : 16 * sm_count), dim3(kJoinThreads), 0, stream, d);
+}
+
+}  // namespace mt

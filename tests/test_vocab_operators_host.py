@@ -60,3 +60,33 @@ def test_gradient_workspace(lib):
     (dict(counter_dev=A + 4), INVALID), (dict(rows=0, x=0, y=0), 0), (dict(cols=0, x=0, y=0), 0)])
 def test_dropout(lib, change, want):
     assert call(lib, "mt_kernel_dropout", DROPOUT, **change) == want
+
+
+LOSS = dict(x=A, w=A, bias=A, labels=A, loss=A, lse=A, rows=4, vocab=90, hidden=64, x_stride=64, w_stride=64, ws=A, ws_bytes=1 << 24, status=0, stream=0)
+LOSS_GRAD = dict(x=A, w=A, bias=A, labels=A, lse=A, grad_loss=A, dx=A, dw=A, db=A, rows=4, vocab=90, hidden=64, x_stride=64, w_stride=64,
+                 dx_stride=64, dw_stride=64, accumulate=0, ws=A, ws_bytes=1 << 26, status=0, stream=0)
+LOSS_SIZES = [(dict(rows=-1), SHAPE), (dict(rows=(1 << 22) + 1), SHAPE), (dict(vocab=0), SHAPE), (dict(vocab=(1 << 22) + 1), SHAPE), (dict(hidden=0), SHAPE),
+              (dict(hidden=60), SHAPE), (dict(hidden=16392, x_stride=16392, w_stride=16392), SHAPE), (dict(x_stride=56), SHAPE), (dict(w_stride=68), SHAPE),
+              (dict(x_stride=-64), SHAPE), (dict(x=0), INVALID), (dict(w=0), INVALID), (dict(labels=0), INVALID), (dict(lse=0), INVALID),
+              (dict(x=A + 8), INVALID), (dict(w=A + 2), INVALID), (dict(bias=A + 4), INVALID), (dict(labels=A + 1), INVALID), (dict(lse=A + 2), INVALID),
+              (dict(ws=0), INVALID), (dict(ws=A + 128), INVALID), (dict(ws_bytes=1000), INVALID)]
+
+
+@pytest.mark.parametrize("change,want", LOSS_SIZES + [(dict(loss=0), INVALID), (dict(loss=A + 2), INVALID), (dict(rows=0, x=0, labels=0, loss=0, ws=0), 0)])
+def test_loss(lib, change, want):
+    assert call(lib, "mt_kernel_vocab_loss", LOSS, **change) == want
+
+
+@pytest.mark.parametrize("change,want", LOSS_SIZES + [
+    (dict(dx=0, dw=0, db=0), INVALID), (dict(dx_stride=60), SHAPE), (dict(dw_stride=32), SHAPE), (dict(dx=A + 8), INVALID), (dict(dw=A + 2), INVALID),
+    (dict(db=A + 2), INVALID), (dict(grad_loss=A + 2), INVALID), (dict(rows=0, accumulate=1, x=0, ws=0), 0)])
+def test_loss_gradient(lib, change, want):
+    assert call(lib, "mt_kernel_vocab_loss_grad", LOSS_GRAD, **change) == want
+
+
+def test_loss_workspaces(lib):
+    for size in (lib.mt_kernel_vocab_loss_workspace, lib.mt_kernel_vocab_loss_grad_workspace):
+        assert size(-1, 9, 16) == 0 and size(4, 0, 16) == 0 and size(4, 9, 12) == 0 and size(4, 9, 0) == 0
+        assert 0 < size(1, 1, 8) <= size(1, 30522, 768) <= size(256, 30522, 768)
+    # the logits are not kept: a fraction of their fp32 size, in bf16 pieces
+    assert lib.mt_kernel_vocab_loss_grad_workspace(8192, 131072, 1024) < 8192 * 131072 * 4 / 8
