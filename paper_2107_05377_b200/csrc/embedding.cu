@@ -7,6 +7,7 @@
 // flight per lane.  The gradient adds up rows in an order that depends on the ids alone, so that equal calls give equal bits: the
 // tokens are sorted by id (stably), every run of equal ids is summed in order of the tokens in fp32, and rounded once.
 //
+// Up to 1024 tokens one launch does it all (embedding_grad_few_kernel).  More:
 //   sort   one cluster sorts (id, token) by least significant digits; every step between its CTAs goes through distributed shared
 //          memory, so that all passes are one launch.  The other CTAs of the launch write the zeros of the rows without a token
 //          meanwhile (all rows: which ones have none is not known yet).
@@ -24,12 +25,16 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortDigitBits = 9;                     // at most
 constexpr int kSortBins = 1 << kSortDigitBits;
-constexpr int kSortMaxCluster = 8;
+constexpr int kSortMaxCluster = 16;                   // (more than the portable eight)
 // counters of every warp, totals of this CTA (two passes in turn), first places of the digits, warp sums of a scan
 constexpr int kSortSmemBytes = (kSortWarps * kSortBins + 2 * kSortBins + kSortBins + kSortWarps) * 4;
+constexpr int kSortUnroll = 8;                        // rounds of a warp whose loads are in flight at a time
 constexpr int kSumColumns = 8;                        // columns of a thread
 constexpr int kSumUnroll = 8;                         // rows asked for at a time
-constexpr int kJoinGroups = 8;                        // row groups of a CTA of the join, 32 threads each
+constexpr int kJoinGroups = 8;                        // warps of a CTA of the join
+constexpr int kFewTokens = 1024;                      // that one launch takes without a sort
+constexpr int kFewBlocks = 4;                         // of 256 columns, that a warp sums at a time
+constexpr int kFewRows = 64;                          // of the table, that a CTA marks at a time
 
 // ---- eight consecutive elements ----------------------------------------------------------------
 // VEC: both addresses are 16-byte aligned and all eight exist; otherwise n of them, one by one.
@@ -120,8 +125,20 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_lookup_kernel(const 
 
 // ---- sort ----------------------------------------------------------------------------------------
 
-// Lanes of the warp that hold the same digit (of those in `active`).
-__device__ __forceinline__ uint32_t same_digit(uint32_t active, uint32_t digit) { return __match_any_sync(active, digit); }
+// Lanes of `active` that hold the same digit: one vote per bit.  (match.any takes some 240 clocks of the warp here: 131072 tokens on eight
+// SMs were sorted in 76 us with it and in 57 with votes.)
+__device__ __forceinline__ uint32_t same_digit(uint32_t active, uint32_t digit, int bits) {
+  uint32_t same = active;
+#pragma unroll
+  for (int b = 0; b < kSortDigitBits; ++b) {
+    if (b < bits) {
+      const bool one = (digit >> b) & 1u;
+      const uint32_t ones = __ballot_sync(active, one);
+      same &= one ? ones : ~ones;
+    }
+  }
+  return same;
+}
 
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr) {
   uint32_t v;
@@ -151,6 +168,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
     if (p.vectors && p.table_stride == p.hidden) {
       uint4* flat = reinterpret_cast<uint4*>(table);
       const int64_t n = static_cast<int64_t>(p.vocab) * p.hidden * sizeof(O) / 16;
+#pragma unroll 4
       for (int64_t i = static_cast<int64_t>(fill) * kSortThreads + tid; i < n; i += static_cast<int64_t>(n_fill) * kSortThreads)
         flat[i] = make_uint4(0, 0, 0, 0);
     } else {
@@ -171,27 +189,35 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
   uint32_t* my_counts = counts + warp * kSortBins;
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * p.digit_bits;
-    const uint32_t* src_key = p.keys[(pass + 1) & 1];
-    const uint32_t* src_token = p.order[(pass + 1) & 1];
-    uint32_t* dst_key = p.keys[pass & 1];
-    uint32_t* dst_token = p.order[pass & 1];
-    auto key_at = [&](int i) -> uint32_t {
-      if (pass != 0) return __ldcg(src_key + i);                   // (written by the other CTAs of the cluster: not through L1)
+    const uint2* src = p.list[(pass + 1) & 1];
+    uint2* dst = p.list[pass & 1];
+    // (id, token) at place i of the list as it is before this pass
+    auto entry = [&](int i) -> uint2 {
+      if (pass != 0) return __ldcg(src + i);                       // (written by the other CTAs of the cluster: not through L1)
       const int id = p.ids[i];
-      return id < 0 || id >= p.vocab || id == p.padding_id ? static_cast<uint32_t>(p.vocab) : static_cast<uint32_t>(id);
+      return make_uint2(id < 0 || id >= p.vocab || id == p.padding_id ? static_cast<uint32_t>(p.vocab) : static_cast<uint32_t>(id),
+                        static_cast<uint32_t>(i));
     };
     for (int b = lane; b < bins; b += 32) my_counts[b] = 0;
     __syncwarp();
-    for (int i0 = begin; i0 < end; i0 += 32) {
-      const int i = i0 + lane;
-      const uint32_t active = __ballot_sync(0xffffffffu, i < end);
-      if (i < end) {
-        if (pass == 0 && p.status != nullptr && p.ids[i] >= p.vocab) atomicOr(p.status, kFlagBadToken);
-        const uint32_t digit = (key_at(i) >> shift) & (bins - 1);
-        const uint32_t same = same_digit(active, digit);
-        if (lane == __ffs(same) - 1) my_counts[digit] += __popc(same);
+    // up to 32 * kSortUnroll entries of a warp stay in registers from the count to their places
+    uint2 e[kSortUnroll];
+    auto fetch = [&](int i0) {
+#pragma unroll
+      for (int u = 0; u < kSortUnroll; ++u) {
+        const int i = i0 + 32 * u + lane;
+        e[u] = i < end ? entry(i) : make_uint2(0, 0);
       }
-      __syncwarp();
+    };
+    for (int i0 = begin; i0 < end; i0 += 32 * kSortUnroll) {
+      fetch(i0);
+#pragma unroll
+      for (int u = 0; u < kSortUnroll; ++u) {
+        const int i = i0 + 32 * u + lane;
+        if (i >= end) continue;
+        if (pass == 0 && p.status != nullptr && p.ids[i] >= p.vocab) atomicOr(p.status, kFlagBadToken);
+        atomicAdd(&my_counts[(e[u].x >> shift) & (bins - 1)], 1u);   // (of this warp: whole numbers, any order)
+      }
     }
     __syncthreads();
     // counts -> places before this warp's among the CTA's; totals of the CTA
@@ -214,10 +240,13 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
     __syncwarp();
     cluster_sync_all();
     if (tid < bins) {
-      for (int r = 0; r < n_ctas; ++r) {
-        const uint32_t c = ld_cluster_u32(map_to_cta(smem_u32(my_totals + tid), r));
-        all += c;
-        if (r < rank) before += c;
+      uint32_t c[kSortMaxCluster];                    // (all asked for before the first is used)
+#pragma unroll
+      for (int r = 0; r < kSortMaxCluster; ++r) c[r] = r < n_ctas ? ld_cluster_u32(map_to_cta(smem_u32(my_totals + tid), r)) : 0u;
+#pragma unroll
+      for (int r = 0; r < kSortMaxCluster; ++r) {
+        all += c[r];
+        if (r < rank) before += c[r];
       }
     }
     // places of the digits before this one, over the whole list
@@ -235,21 +264,22 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
       first[tid] = lower + scan - all + before;
     }
     __syncthreads();
-    for (int i0 = begin; i0 < end; i0 += 32) {
-      const int i = i0 + lane;
-      const uint32_t active = __ballot_sync(0xffffffffu, i < end);
-      if (i < end) {
-        const uint32_t key = key_at(i);
-        const uint32_t token = pass == 0 ? static_cast<uint32_t>(i) : __ldcg(src_token + i);
-        const uint32_t digit = (key >> shift) & (bins - 1);
-        const uint32_t same = same_digit(active, digit);
-        const uint32_t place = first[digit] + my_counts[digit] + __popc(same & ((1u << lane) - 1));
-        __syncwarp(active);
-        if (lane == __ffs(same) - 1) my_counts[digit] += __popc(same);
-        dst_key[place] = key;
-        dst_token[place] = token;
+    for (int i0 = begin; i0 < end; i0 += 32 * kSortUnroll) {
+      if (end - begin > 32 * kSortUnroll) fetch(i0);
+#pragma unroll
+      for (int u = 0; u < kSortUnroll; ++u) {
+        const bool there = i0 + 32 * u + lane < end;
+        const uint32_t active = __ballot_sync(0xffffffffu, there);
+        if (there) {
+          const uint32_t digit = (e[u].x >> shift) & (bins - 1);
+          const uint32_t same = same_digit(active, digit, p.digit_bits);
+          const uint32_t place = first[digit] + my_counts[digit] + __popc(same & ((1u << lane) - 1));
+          __syncwarp(active);
+          if (lane == __ffs(same) - 1) my_counts[digit] += __popc(same);
+          dst[place] = e[u];
+        }
+        __syncwarp();
       }
-      __syncwarp();
     }
     // the next pass reads what the other CTAs have written (and no CTA leaves while another reads its totals)
     __syncwarp();
@@ -259,55 +289,109 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
 
 // ---- sum -----------------------------------------------------------------------------------------
 
+// Eight columns of a row as they lie in memory.
+template <typename T> struct Raw;
+template <> struct Raw<bf16> { uint4 a; };
+template <> struct Raw<float> { uint4 a, b; };
+template <bool VEC>
+__device__ __forceinline__ void load_raw(const bf16* p, int n, Raw<bf16>& r) {
+  if (VEC) {
+    r.a = __ldg(reinterpret_cast<const uint4*>(p));
+  } else {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = i < n ? __bfloat16_as_ushort(p[i]) : 0u;
+    r.a = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load_raw(const float* p, int n, Raw<float>& r) {
+  if (VEC) {
+    r.a = __ldg(reinterpret_cast<const uint4*>(p));
+    r.b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+  } else {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = i < n ? __float_as_uint(p[i]) : 0u;
+    r.a = make_uint4(w[0], w[1], w[2], w[3]);
+    r.b = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+__device__ __forceinline__ void add_raw(const Raw<bf16>& r, float (&f)[8]) {
+  const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[2 * i] += bf16_lo(w[i]); f[2 * i + 1] += bf16_hi(w[i]); }
+}
+__device__ __forceinline__ void add_raw(const Raw<float>& r, float (&f)[8]) {
+  const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] += __uint_as_float(w[i]);
+}
+
+// scale * sum (+ what is there) to eight columns of the table's gradient.
+template <bool VEC, typename O>
+__device__ __forceinline__ void finish8(const EmbeddingGradParams& p, int64_t row, int col, float (&acc)[8]) {
+  O* out = static_cast<O*>(p.grad_table) + row * p.table_stride + col;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] *= p.scale;
+  if (p.accumulate) add_present8<VEC>(out, p.hidden - col, acc);
+  store8<VEC>(out, p.hidden - col, acc);
+}
+
 template <typename G, typename O, bool VEC>
 __global__ void __launch_bounds__(128) embedding_grad_sum_kernel(const __grid_constant__ EmbeddingGradParams p) {
   __shared__ uint32_t s_key[kEmbeddingMaxChunk + 2];     // one before the chunk, the chunk, one behind it
   __shared__ uint32_t s_token[kEmbeddingMaxChunk];
+  __shared__ int s_count;
   grid_dependency_wait();
   grid_launch_dependents();
   const int n = p.tokens, len = p.chunk;
   const int e0 = blockIdx.x * len;
-  const int count = min(len, n - e0);
-  const uint32_t* keys = p.keys[(p.passes - 1) & 1];
-  const uint32_t* order = p.order[(p.passes - 1) & 1];
+  const int listed = min(len, n - e0);
+  const uint2* list = p.list[(p.passes - 1) & 1];
   constexpr uint32_t kNone = 0xffffffffu;                // (no id)
-  for (int i = threadIdx.x; i < count + 2; i += blockDim.x) {
-    const int e = e0 - 1 + i;
-    s_key[i] = e < 0 || e >= n ? kNone : keys[e];
-  }
-  for (int i = threadIdx.x; i < count; i += blockDim.x) s_token[i] = order[e0 + i];
+  const uint32_t none = static_cast<uint32_t>(p.vocab);  // (tokens without a part, at the end of the list)
+  if (threadIdx.x == 0) s_count = 0;
   __syncthreads();
+  int mine = 0;
+  for (int i = threadIdx.x; i < listed + 2; i += blockDim.x) {
+    const int e = e0 - 1 + i;
+    const uint2 at = e < 0 || e >= n ? make_uint2(kNone, 0) : list[e];
+    s_key[i] = at.x;
+    if (i >= 1 && i <= listed) {
+      s_token[i - 1] = at.y;
+      mine += at.x != none ? 1 : 0;
+    }
+  }
+  if (mine != 0) atomicAdd(&s_count, mine);
+  __syncthreads();
+  const int count = s_count;
   const int col = (blockIdx.y * blockDim.x + threadIdx.x) * kSumColumns;
-  if (col >= p.hidden) return;
+  if (col >= p.hidden || count == 0) return;
   const int left = p.hidden - col;
   const G* grad = static_cast<const G*>(p.grad_out) + col;
   float acc[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) acc[j] = 0.f;
   bool began_here = s_key[0] != s_key[1];
-  const uint32_t none = static_cast<uint32_t>(p.vocab);
-  for (int i0 = 0; i0 < count && s_key[i0 + 1] != none; i0 += kSumUnroll) {
-    float f[kSumUnroll][8];
+  for (int i0 = 0; i0 < count; i0 += kSumUnroll) {
+    Raw<G> row[kSumUnroll];
 #pragma unroll
     for (int u = 0; u < kSumUnroll; ++u) {
-      const int i = i0 + u;
-      if (i < count && s_key[i + 1] != none) load8<VEC>(grad + static_cast<int64_t>(s_token[i]) * p.grad_stride, left, f[u]);
+      // (behind the last one: it once more, unused)
+      const int i = min(i0 + u, count - 1);
+      load_raw<VEC>(grad + static_cast<int64_t>(s_token[i]) * p.grad_stride, left, row[u]);
     }
 #pragma unroll
     for (int u = 0; u < kSumUnroll; ++u) {
       const int i = i0 + u;
-      if (i >= count || s_key[i + 1] == none) break;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += f[u][j];
+      if (i >= count) break;
+      add_raw(row[u], acc);
       const uint32_t key = s_key[i + 1];
       const bool ends = s_key[i + 2] != key;
       if (!ends && i + 1 < count) continue;
       if (began_here && ends) {
-        O* out = static_cast<O*>(p.grad_table) + static_cast<int64_t>(key) * p.table_stride + col;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] *= p.scale;
-        if (p.accumulate) add_present8<VEC>(out, left, acc);
-        store8<VEC>(out, left, acc);
+        finish8<VEC, O>(p, key, col, acc);
       } else {
         // (slot 0: of a run that began before this chunk; slot 1: of one that begins here and goes on)
         float* part = p.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (began_here ? 1 : 0)) * p.part_stride + col;
@@ -320,55 +404,231 @@ __global__ void __launch_bounds__(128) embedding_grad_sum_kernel(const __grid_co
   }
 }
 
-// A CTA per chunk (and 256 columns): if a run begins in this chunk and goes on behind it, adds up its parts.  Eight groups of threads
-// take every eighth part each, then their sums are added in order.
+// The parts of every run that crosses a border, in order.  A warp per chunk looks whether a run begins there and goes on behind it, and
+// how far (the chunks' first ids are sorted: 32 of them are tried at a time).  Of few parts the warp takes the sum alone; of more, the
+// CTA's eight warps take every eighth part each, and their sums are added in order.  256 columns to a CTA.
 template <typename O, bool VEC>
 __global__ void __launch_bounds__(32 * kJoinGroups) embedding_grad_join_kernel(const __grid_constant__ EmbeddingGradParams p) {
   __shared__ float s_acc[kJoinGroups][32][9];
+  __shared__ int s_behind[kJoinGroups];
+  __shared__ uint32_t s_key[kJoinGroups];
   grid_dependency_wait();
   grid_launch_dependents();
   const int n = p.tokens, len = p.chunk;
-  const int e0 = blockIdx.x * len, e1 = e0 + len;
-  if (e1 >= n) return;                                    // (the last chunk: nothing goes on behind it)
-  const uint32_t* keys = p.keys[(p.passes - 1) & 1];
-  const uint32_t key = keys[e1 - 1];
-  if (key == static_cast<uint32_t>(p.vocab) || keys[e1] != key || (e0 > 0 && keys[e0 - 1] == key)) return;
-  // chunks behind this one that the run reaches: those that begin with its id (the ids are sorted)
-  int behind = 0;
-  for (int64_t c0 = blockIdx.x + 1; ; c0 += blockDim.x) {
-    const int64_t e = (c0 + threadIdx.x) * len;
-    const int got = __syncthreads_count(e < n && keys[e] == key);
-    behind += got;
-    if (got < static_cast<int>(blockDim.x)) break;
-  }
+  const int chunks = (n + len - 1) / len;
+  const uint2* list = p.list[(p.passes - 1) & 1];
   const int group = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int col = (blockIdx.y * 32 + lane) * kSumColumns;
-  float acc[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-  if (col < p.hidden) {
-    const float* parts = p.parts + static_cast<int64_t>(blockIdx.x) * 2 * p.part_stride + col;
-#pragma unroll 4
-    for (int i = group; i <= behind; i += kJoinGroups) {  // part 0: slot 1 of this chunk; part i: slot 0 of the i-th behind it
-      float f[8];
-      load8<true>(parts + (i == 0 ? p.part_stride : static_cast<int64_t>(i) * 2 * p.part_stride), 8, f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += f[j];
+  const int chunk = blockIdx.x * kJoinGroups + group;
+  const int64_t e0 = static_cast<int64_t>(chunk) * len, e1 = e0 + len;
+  int behind = 0;                                         // chunks behind this one that the run reaches
+  uint32_t key = 0;
+  if (e1 < n) {                                           // (behind the last chunk nothing goes on)
+    // lane 0: the entry before the chunk; 1: its last; 2 and on: the first of each of the next thirty
+    const int64_t at = lane == 0 ? e0 - 1 : (lane == 1 ? e1 - 1 : e1 + static_cast<int64_t>(lane - 2) * len);
+    const uint32_t seen = at >= 0 && at < n ? list[at].x : 0xffffffffu;
+    key = __shfl_sync(0xffffffffu, seen, 1);
+    const uint32_t same = __ballot_sync(0xffffffffu, seen == key);
+    if (key != static_cast<uint32_t>(p.vocab) && (same & 1u) == 0) {
+      behind = __popc(same >> 2);
+      if (behind == 30) {
+        // chunks [low, high) behind: the first id of low - 1 is the run's, that of high is not (or there is none)
+        int low = chunk + 31, high = chunks;
+        while (low < high) {
+          const int step = (high - low + 31) / 32;
+          const int64_t c = low + static_cast<int64_t>(lane) * step;
+          const uint32_t hits = __ballot_sync(0xffffffffu, c < high && list[c * len].x == key);
+          const int n_hits = __popc(hits);
+          if (n_hits < 32 && low + static_cast<int64_t>(n_hits) * step < high) high = low + n_hits * step;
+          if (n_hits > 0) low += (n_hits - 1) * step + 1;
+        }
+        behind = low - 1 - chunk;
+      }
     }
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) s_acc[group][lane][j] = acc[j];
-  __syncthreads();
-  if (group != 0 || col >= p.hidden) return;
-  for (int g = 1; g < kJoinGroups; ++g) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += s_acc[g][lane][j];
+  if (lane == 0) {
+    s_behind[group] = behind;
+    s_key[group] = key;
   }
-  O* out = static_cast<O*>(p.grad_table) + static_cast<int64_t>(key) * p.table_stride + col;
+  const int col = (blockIdx.y * 32 + lane) * kSumColumns;
+  const bool in_row = col < p.hidden;
+  float acc[8];
+  // part 0: slot 1 of the chunk; part i: slot 0 of the i-th behind it
+  auto add_part = [&](int c, int i) {
+    float f[8];
+    load8<true>(p.parts + (static_cast<int64_t>(c + i) * 2 + (i == 0 ? 1 : 0)) * p.part_stride + col, 8, f);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] *= p.scale;
-  if (p.accumulate) add_present8<VEC>(out, p.hidden - col, acc);
-  store8<VEC>(out, p.hidden - col, acc);
+    for (int j = 0; j < 8; ++j) acc[j] += f[j];
+  };
+  if (behind > 0 && behind < 2 * kJoinGroups && in_row) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+#pragma unroll 8
+    for (int i = 0; i <= behind; ++i) add_part(chunk, i);
+    finish8<VEC, O>(p, key, col, acc);
+  }
+  __syncthreads();
+  for (int g = 0; g < kJoinGroups; ++g) {
+    const int far = s_behind[g];
+    if (far < 2 * kJoinGroups) continue;                  // (the same for all threads)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    if (in_row) {
+#pragma unroll 8
+      for (int i = group; i <= far; i += kJoinGroups) add_part(blockIdx.x * kJoinGroups + g, i);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s_acc[group][lane][j] = acc[j];
+    __syncthreads();
+    if (group == 0 && in_row) {
+      for (int w = 1; w < kJoinGroups; ++w) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += s_acc[w][lane][j];
+      }
+      finish8<VEC, O>(p, s_key[g], col, acc);
+    }
+    __syncthreads();
+  }
+}
+
+// ---- few tokens ------------------------------------------------------------------------------------
+
+// Up to kFewTokens tokens in one launch, without a sort: every CTA keeps all ids in shared memory.  CTA t < tokens looks whether token
+// t is the first of its id; if so it lists the others in order and sums their rows: with one token a warp per block of 256 columns,
+// with more the eight warps take every eighth row each and are added in order.  The CTAs behind write the zeros of
+// the rows that no id names, a range of rows each.
+template <typename G, typename O, bool VEC>
+__global__ void __launch_bounds__(32 * kJoinGroups) embedding_grad_few_kernel(const __grid_constant__ EmbeddingGradParams p) {
+  constexpr int THREADS = 32 * kJoinGroups, PER = kFewTokens / THREADS;
+  static_assert(kFewTokens % THREADS == 0, "every thread looks at the same number of ids");
+  __shared__ int s_id[kFewTokens];
+  __shared__ int s_list[kFewTokens];
+  __shared__ int s_warp[kJoinGroups];
+  __shared__ uint32_t s_named[kFewRows / 32];
+  __shared__ float s_acc[kFewBlocks][kJoinGroups][8][32];
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = p.tokens;
+  for (int i = tid; i < kFewTokens; i += THREADS) {
+    const int id = i < n ? p.ids[i] : -1;
+    if (blockIdx.x == 0 && id >= p.vocab && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
+    s_id[i] = id < 0 || id >= p.vocab || id == p.padding_id ? -1 : id;
+  }
+  __syncthreads();
+  if (static_cast<int>(blockIdx.x) >= n) {
+    // zeros: kFewRows rows at a time, those that are named marked first
+    O* table = static_cast<O*>(p.grad_table);
+    const int fill = blockIdx.x - n, n_fill = gridDim.x - n;
+    for (int64_t v0 = static_cast<int64_t>(fill) * kFewRows; v0 < p.vocab; v0 += static_cast<int64_t>(n_fill) * kFewRows) {
+      for (int i = tid; i < kFewRows / 32; i += THREADS) s_named[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < n; i += THREADS) {
+        const int64_t at = s_id[i] - v0;
+        if (s_id[i] >= 0 && at >= 0 && at < kFewRows) atomicOr(&s_named[at >> 5], 1u << (at & 31));
+      }
+      __syncthreads();
+      for (int r = warp; r < kFewRows && v0 + r < p.vocab; r += kJoinGroups) {
+        if ((s_named[r >> 5] >> (r & 31)) & 1u) continue;
+        O* row = table + (v0 + r) * p.table_stride;
+        if (VEC) {
+          for (int c = lane; c < p.hidden * static_cast<int>(sizeof(O)) / 16; c += 32) reinterpret_cast<uint4*>(row)[c] = make_uint4(0, 0, 0, 0);
+        } else {
+          for (int c = lane; c < p.hidden; c += 32) row[c] = O(0.f);
+        }
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  const int token = blockIdx.x;
+  const int id = s_id[token];
+  if (id < 0) return;
+  // ids [tid * PER, ...): how many are this one, whether one of them comes before the token
+  int hits = 0;
+  bool before = false;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = tid * PER + k;
+    if (s_id[i] == id) {
+      ++hits;
+      before |= i < token;
+    }
+  }
+  if (__syncthreads_or(before)) return;
+  int places = hits;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int other = __shfl_up_sync(0xffffffffu, places, o);
+    if (lane >= o) places += other;
+  }
+  if (lane == 31) s_warp[warp] = places;
+  __syncthreads();
+  int count = 0;
+  places -= hits;
+  for (int w = 0; w < kJoinGroups; ++w) {
+    if (w < warp) places += s_warp[w];
+    count += s_warp[w];
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = tid * PER + k;
+    if (s_id[i] == id) s_list[places++] = i;
+  }
+  __syncthreads();
+  const G* grad = static_cast<const G*>(p.grad_out);
+  const int blocks = (p.hidden + 255) / 256;
+  float acc[8];
+  if (count == 1) {
+    for (int b = warp; b < blocks; b += kJoinGroups) {
+      const int col = b * 256 + lane * 8;
+      if (col >= p.hidden) continue;
+      Raw<G> r;
+      load_raw<VEC>(grad + token * p.grad_stride + col, p.hidden - col, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+      add_raw(r, acc);
+      finish8<VEC, O>(p, id, col, acc);
+    }
+    return;
+  }
+  for (int b0 = 0; b0 < blocks; b0 += kFewBlocks) {
+    float sum[kFewBlocks][8];
+#pragma unroll
+    for (int b = 0; b < kFewBlocks; ++b) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[b][j] = 0.f;
+    }
+#pragma unroll 2
+    for (int i = warp; i < count; i += kJoinGroups) {
+      Raw<G> r[kFewBlocks];
+      const G* row = grad + s_list[i] * p.grad_stride;
+#pragma unroll
+      for (int b = 0; b < kFewBlocks; ++b) {
+        const int col = (b0 + b) * 256 + lane * 8;
+        if (col < p.hidden) load_raw<VEC>(row + col, p.hidden - col, r[b]);
+      }
+#pragma unroll
+      for (int b = 0; b < kFewBlocks; ++b) {
+        if ((b0 + b) * 256 + lane * 8 < p.hidden) add_raw(r[b], sum[b]);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < kFewBlocks; ++b) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s_acc[b][warp][j][lane] = sum[b][j];
+    }
+    __syncthreads();
+    if (warp < kFewBlocks && (b0 + warp) * 256 + lane * 8 < p.hidden) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinGroups; ++w) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += s_acc[warp][w][j][lane];
+      }
+      finish8<VEC, O>(p, id, (b0 + warp) * 256 + lane * 8, acc);
+    }
+    __syncthreads();
+  }
 }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -389,20 +649,51 @@ cudaError_t launch_sum_join(const EmbeddingGradParams& p, bool vec, cudaStream_t
                                 dim3(chunks, (units + threads - 1) / threads), dim3(threads), 0, stream, p);
   if (e != cudaSuccess || chunks < 2) return e;
   return launch_kernel(vec ? embedding_grad_join_kernel<O, true> : embedding_grad_join_kernel<O, false>,
-                       dim3(chunks, (units + 31) / 32), dim3(32 * kJoinGroups), 0, stream, p);
+                       dim3((chunks + kJoinGroups - 1) / kJoinGroups, (units + 31) / 32), dim3(32 * kJoinGroups), 0, stream, p);
+}
+
+template <typename G, typename O>
+cudaError_t launch_few(const EmbeddingGradParams& p, bool vec, int sm_count, cudaStream_t stream) {
+  int64_t fill = 0;
+  if (!p.accumulate) fill = (static_cast<int64_t>(p.vocab) + kFewRows - 1) / kFewRows;
+  if (fill > 4 * sm_count) fill = 4 * sm_count;
+  if (p.tokens + fill == 0) return cudaSuccess;
+  return launch_kernel(vec ? embedding_grad_few_kernel<G, O, true> : embedding_grad_few_kernel<G, O, false>,
+                       dim3(static_cast<unsigned>(p.tokens + fill)), dim3(32 * kJoinGroups), 0, stream, p);
 }
 
 template <typename O>
 cudaError_t launch_sort(EmbeddingGradParams* p, int sm_count, cudaStream_t stream) {
   auto kernel = token_sort_kernel<O>;
   static PerDeviceOnce once;   // per instantiation
-  cudaError_t err = per_device_once(once, [&](int) {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmemBytes);
-  });
+  static int most_ctas[kMaxDevices];
+  int device = 0;
+  cudaError_t err = per_device_once(once, [&](int dev) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmemBytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSortMaxCluster);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = kSortSmemBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kSortMaxCluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+    most_ctas[dev] = e == cudaSuccess && clusters > 0 ? kSortMaxCluster : 8;
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return cudaSuccess;
+  }, &device);
   if (err != cudaSuccess) return err;
-  // a CTA of the cluster per two rounds of all its warps, as far as eight of them
+  // A CTA of the cluster per round of all its warps, as far as sixteen of them (where so many fit; else eight).  What a pass costs is
+  // its stores, 32 places per warp that lie anywhere: one per clock and SM.  131072 tokens: 76 us with match.any and ids and tokens
+  // stored apart, eight CTAs; 57 with votes; 28 with one store for both, sixteen CTAs and the entries kept in registers.
   int ctas = 1;
-  while (ctas < kSortMaxCluster && static_cast<int64_t>(ctas) * 2 * kSortThreads < p->tokens) ctas *= 2;
+  while (ctas < most_ctas[device] && static_cast<int64_t>(ctas) * kSortThreads < p->tokens) ctas *= 2;
   p->sort_ctas = ctas;
   int fill = 0;
   if (!p->accumulate) {
@@ -435,12 +726,16 @@ int embedding_grad_chunk(int tokens) {
 cudaError_t launch_embedding_grad(EmbeddingGradParams p, bool grad_f32, bool out_f32, int sm_count, cudaStream_t stream) {
   const bool vec = p.hidden % 8 == 0 && p.table_stride % 8 == 0 && p.grad_stride % 8 == 0 && aligned16(p.grad_out) && aligned16(p.grad_table);
   p.vectors = vec ? 1 : 0;
+  if (p.tokens <= kFewTokens) {
+    if (grad_f32) return out_f32 ? launch_few<float, float>(p, vec, sm_count, stream) : launch_few<float, bf16>(p, vec, sm_count, stream);
+    return out_f32 ? launch_few<bf16, float>(p, vec, sm_count, stream) : launch_few<bf16, bf16>(p, vec, sm_count, stream);
+  }
   int bits = 1;                              // of the largest key, which is `vocab`
   while (bits < 31 && (p.vocab >> bits) != 0) ++bits;
   p.passes = (bits + kSortDigitBits - 1) / kSortDigitBits;
   p.digit_bits = (bits + p.passes - 1) / p.passes;
   cudaError_t e = out_f32 ? launch_sort<float>(&p, sm_count, stream) : launch_sort<bf16>(&p, sm_count, stream);
-  if (e != cudaSuccess || p.tokens == 0) return e;
+  if (e != cudaSuccess) return e;
   if (grad_f32) return out_f32 ? launch_sum_join<float, float>(p, vec, stream) : launch_sum_join<float, bf16>(p, vec, stream);
   return out_f32 ? launch_sum_join<bf16, float>(p, vec, stream) : launch_sum_join<bf16, bf16>(p, vec, stream);
 }

@@ -2463,8 +2463,8 @@ int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* 
              ? MT_OK : MT_ERR_CUDA;
 }
 
-// Workspace: four lists of the tokens, then the parts of every chunk.
-static size_t embedding_list_bytes(int32_t tokens) { return whole_lines(static_cast<size_t>(tokens) * 4); }
+// Workspace: two lists of (id, token), then the parts of every chunk.
+static size_t embedding_list_bytes(int32_t tokens) { return whole_lines(static_cast<size_t>(tokens) * 8); }
 static int64_t embedding_part_stride(int32_t hidden) { return (static_cast<int64_t>(hidden) + 7) / 8 * 8; }
 
 size_t mt_kernel_embedding_grad_workspace(int32_t tokens, int32_t vocab, int32_t hidden) {
@@ -2472,7 +2472,7 @@ size_t mt_kernel_embedding_grad_workspace(int32_t tokens, int32_t vocab, int32_t
   if (tokens == 0) return 256;
   const int chunk = embedding_grad_chunk(tokens);
   const size_t chunks = (static_cast<size_t>(tokens) + chunk - 1) / chunk;
-  return 4 * embedding_list_bytes(tokens) + whole_lines(chunks * 2 * embedding_part_stride(hidden) * 4);
+  return 2 * embedding_list_bytes(tokens) + whole_lines(chunks * 2 * embedding_part_stride(hidden) * 4);
 }
 
 int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void* d_grad_table, int32_t tokens, int32_t vocab,
@@ -2497,11 +2497,8 @@ int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void*
   p.tokens = tokens; p.vocab = vocab; p.hidden = hidden; p.scale = scale; p.status = d_status;
   p.padding_id = padding_id < 0 ? -1 : padding_id; p.accumulate = accumulate != 0 ? 1 : 0;
   uint8_t* ws = static_cast<uint8_t*>(d_workspace);
-  for (int i = 0; i < 2; ++i) {
-    p.keys[i] = reinterpret_cast<uint32_t*>(ws + (2 * i) * embedding_list_bytes(tokens));
-    p.order[i] = reinterpret_cast<uint32_t*>(ws + (2 * i + 1) * embedding_list_bytes(tokens));
-  }
-  p.parts = reinterpret_cast<float*>(ws + 4 * embedding_list_bytes(tokens));
+  for (int i = 0; i < 2; ++i) p.list[i] = reinterpret_cast<uint2*>(ws + i * embedding_list_bytes(tokens));
+  p.parts = reinterpret_cast<float*>(ws + 2 * embedding_list_bytes(tokens));
   p.part_stride = embedding_part_stride(hidden);
   p.chunk = embedding_grad_chunk(tokens);
   return launch_embedding_grad(p, grad_out_dtype == MT_DTYPE_F32, grad_table_dtype == MT_DTYPE_F32, sms, as_stream(stream)) == cudaSuccess

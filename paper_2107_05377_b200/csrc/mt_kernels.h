@@ -416,9 +416,9 @@ struct EmbeddingGradParams {
   int32_t accumulate;
   float scale;
   uint32_t* status;
-  // workspace: the sorted list, written in turn, and what chunks have of runs that cross their borders ([chunk][2][part_stride])
-  uint32_t* keys[2];
-  uint32_t* order[2];
+  // workspace: the list of (id, token), sorted in turn from one to the other, and what chunks have of runs that cross their borders
+  // ([chunk][2][part_stride])
+  uint2* list[2];
   float* parts;
   int64_t part_stride;
   int32_t chunk;            // embedding_grad_chunk(tokens)

@@ -48,7 +48,7 @@ def test_gradient_workspace(lib):
     assert size(-1, 9, 16) == 0 and size(4, 0, 16) == 0 and size(4, 9, 0) == 0 and size((1 << 30) + 1, 9, 16) == 0
     assert size(0, 9, 16) >= 1
     for tokens in (1, 7, 8, 9, 4096, 131072, 1 << 30):
-        chunks = size(tokens, 9, 8) - 4 * ((tokens * 4 + 255) // 256 * 256)
+        chunks = size(tokens, 9, 8) - 2 * ((tokens * 8 + 255) // 256 * 256)
         assert chunks % 256 == 0 and chunks > 0
     assert size(1 << 30, 9, 1024) > 1 << 33            # (counted in 64 bits)
 
