@@ -250,62 +250,101 @@ def mt_kernel_pooler_head_static(hidden, pool_w, pool_b, cls_w, cls_b, logits, b
 # the vocabulary's ends of a language model, and dropout
 # ---------------------------------------------------------------------------
 
-def _operands(where: str, *tensors) -> int:
-    """Refuses what the library cannot see: tensors that are not on the current device.  Returns that device's index."""
-    import torch
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise MTError(-1, where, f"a tensor is on {t.device}, the current device is cuda:{device}")
-    return device
+class _Torch:
+    """What the calls below need of torch, looked up once: a short call spends more time on this side than on the GPU."""
+
+    def __init__(self):
+        import torch
+        self.dtypes = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+        self.bf16, self.f32, self.i32 = torch.bfloat16, torch.float32, torch.int32
+        self.device = torch.cuda.current_device
+        self.raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _matrix(where: str, t, rows: int, cols: int):
-    """(pointer, dtype code, row stride) of a 2-D tensor with contiguous rows."""
-    import torch
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+_torch: Optional[_Torch] = None
+
+
+def _begin(where: str, stream):
+    """(torch's types, current device, handle of the stream).  A stream of another device is refused."""
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    device = _torch.device()
+    if stream is None:
+        return _torch, device, _torch.raw_stream(device)
+    if stream.device.index != device:
+        raise MTError(-1, where, f"a stream of {stream.device}, the current device is cuda:{device}")
+    return _torch, device, stream.cuda_stream
+
+
+def _elsewhere(where: str, t, device: int) -> MTError:
+    return MTError(-1, where, f"a tensor is on {t.device}, the current device is cuda:{device}")
+
+
+def _matrix(where: str, device: int, t, rows: int, cols: int):
+    """(pointer, dtype code, row stride) of a 2-D tensor with contiguous rows on the current device."""
+    if t.get_device() != device:
+        raise _elsewhere(where, t, device)
+    if t.shape != (rows, cols):
         raise MTError(-2, where, f"expected a {rows} x {cols} tensor, got {tuple(t.shape)}")
-    if t.dtype == torch.bfloat16:
-        dtype = DTYPE_BF16
-    elif t.dtype == torch.float32:
-        dtype = DTYPE_F32
-    else:
+    dtype = _torch.dtypes.get(t.dtype)
+    if dtype is None:
         raise MTError(-7, where, f"dtype {t.dtype}")
     stride, step = t.stride()
     if step != 1 and cols > 1:
         raise MTError(-1, where, "the rows of a tensor are not contiguous")
-    # (the stride of a single row, or of none, says nothing)
-    return t.data_ptr(), dtype, stride if rows > 1 else max(stride, cols)
+    # (nobody walks the stride of a single row, or of none: any that the library takes will do)
+    return t.data_ptr(), dtype, stride if rows > 1 else cols
 
 
-def _vector(where: str, t, n: int, dtype: str) -> int:
-    """Pointer of a contiguous tensor of n elements of a type; 0 for None."""
+def _bf16_matrix(where: str, device: int, t, rows: int, cols: int):
+    pointer, dtype, stride = _matrix(where, device, t, rows, cols)
+    if dtype != DTYPE_BF16:
+        raise MTError(-7, where, f"dtype {t.dtype}")
+    return pointer, stride
+
+
+def _vector(where: str, device: int, t, n: int, dtype) -> int:
+    """Pointer of a contiguous tensor of n elements of a type on the current device; 0 for None."""
     if t is None:
         return 0
-    if t.numel() != n or str(t.dtype) != "torch." + dtype or not t.is_contiguous():
-        raise MTError(-1, where, f"expected {n} contiguous {dtype} elements, got {tuple(t.shape)} {t.dtype}")
+    if t.get_device() != device:
+        raise _elsewhere(where, t, device)
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise MTError(-1, where, f"expected {n} contiguous elements of {dtype}, got {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
 
 
-def _stream_of(device: int, stream) -> int:
-    """The stream's handle; a stream of another device is refused."""
-    import torch
-    if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream
-    if stream.device.index != device:
-        raise MTError(-1, "stream", f"a stream of {stream.device}, the current device is cuda:{device}")
-    return stream.cuda_stream
+def _memory(where: str, device: int, t):
+    """(pointer, bytes) of a contiguous workspace on the current device."""
+    if t.get_device() != device:
+        raise _elsewhere(where, t, device)
+    if not t.is_contiguous():
+        raise MTError(-1, where, "the workspace is not contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _status_word(where: str, device: int, t) -> int:
+    if t is None:
+        return 0
+    if t.get_device() != device:
+        raise _elsewhere(where, t, device)
+    if t.element_size() != 4 or t.numel() < 1:
+        raise MTError(-1, where, "the status is one 32-bit word")
+    return t.data_ptr()
 
 
 def mt_kernel_embedding_lookup(ids, table, out, scale: float = 1.0, status=None, stream=None) -> None:
     """out[t] = scale * table[ids[t]] (ids int32 of any shape, out [ids.numel(), hidden]); zeros for ids < 0."""
     where = "mt_kernel_embedding_lookup"
-    device = _operands(where, ids, table, out, status)
+    torch, device, stream = _begin(where, stream)
     tokens, (vocab, hidden) = ids.numel(), table.shape
-    table_ptr, table_dtype, table_stride = _matrix(where, table, vocab, hidden)
-    out_ptr, out_dtype, out_stride = _matrix(where, out, tokens, hidden)
-    _check(lib().mt_kernel_embedding_lookup(_vector(where, ids, tokens, "int32"), table_ptr, out_ptr, tokens, vocab, hidden, table_stride,
-                                            out_stride, table_dtype, out_dtype, scale, _ptr(status), _stream_of(device, stream)), where)
+    table_ptr, table_dtype, table_stride = _matrix(where, device, table, vocab, hidden)
+    out_ptr, out_dtype, out_stride = _matrix(where, device, out, tokens, hidden)
+    code = lib().mt_kernel_embedding_lookup(_vector(where, device, ids, tokens, torch.i32), table_ptr, out_ptr, tokens, vocab, hidden,
+                                            table_stride, out_stride, table_dtype, out_dtype, scale, _status_word(where, device, status),
+                                            stream)
+    _check(code, where)
 
 
 def mt_kernel_embedding_grad_workspace(tokens: int, vocab: int, hidden: int) -> int:
@@ -316,41 +355,39 @@ def mt_kernel_embedding_grad(ids, grad_out, grad_table, workspace, scale: float 
                              accumulate: bool = False, status=None, stream=None) -> None:
     """grad_table[v] = scale * sum of grad_out[t] over ids[t] == v, zeros where there is none; or added to grad_table."""
     where = "mt_kernel_embedding_grad"
-    device = _operands(where, ids, grad_out, grad_table, workspace, status)
+    torch, device, stream = _begin(where, stream)
     tokens, (vocab, hidden) = ids.numel(), grad_table.shape
-    grad_ptr, grad_dtype, grad_stride = _matrix(where, grad_out, tokens, hidden)
-    table_ptr, table_dtype, table_stride = _matrix(where, grad_table, vocab, hidden)
-    _check(lib().mt_kernel_embedding_grad(_vector(where, ids, tokens, "int32"), grad_ptr, table_ptr, tokens, vocab, hidden, grad_stride,
-                                          table_stride, grad_dtype, table_dtype, scale, padding_id, 1 if accumulate else 0,
-                                          workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(status),
-                                          _stream_of(device, stream)), where)
+    grad_ptr, grad_dtype, grad_stride = _matrix(where, device, grad_out, tokens, hidden)
+    table_ptr, table_dtype, table_stride = _matrix(where, device, grad_table, vocab, hidden)
+    ws_ptr, ws_bytes = _memory(where, device, workspace)
+    code = lib().mt_kernel_embedding_grad(_vector(where, device, ids, tokens, torch.i32), grad_ptr, table_ptr, tokens, vocab, hidden,
+                                          grad_stride, table_stride, grad_dtype, table_dtype, scale, padding_id, 1 if accumulate else 0,
+                                          ws_ptr, ws_bytes, _status_word(where, device, status), stream)
+    _check(code, where)
 
 
 def mt_kernel_dropout(x, y, p: float, seed: int, counter: int = 0, residual=None, counter_dev=None, stream=None) -> None:
     """y = residual + x * keep / (1 - p), keep from (seed, counter, row, column); ``counter_dev``: an int64 or uint64 device
     tensor of one element that is added to ``counter`` when the call runs."""
     where = "mt_kernel_dropout"
-    device = _operands(where, x, y, residual, counter_dev)
+    torch, device, stream = _begin(where, stream)
     rows, cols = x.shape
-    x_ptr, x_dtype, x_stride = _matrix(where, x, rows, cols)
-    y_ptr, y_dtype, y_stride = _matrix(where, y, rows, cols)
-    r_ptr, r_stride = 0, 0
+    x_ptr, x_dtype, x_stride = _matrix(where, device, x, rows, cols)
+    y_ptr, y_dtype, y_stride = _matrix(where, device, y, rows, cols)
+    r_ptr, r_stride, c_ptr = 0, 0, 0
     if residual is not None:
-        r_ptr, r_dtype, r_stride = _matrix(where, residual, rows, cols)
+        r_ptr, r_dtype, r_stride = _matrix(where, device, residual, rows, cols)
         if r_dtype != y_dtype:
             raise MTError(-1, where, "residual and y have different types")
-    if counter_dev is not None and (counter_dev.numel() != 1 or counter_dev.element_size() != 8 or counter_dev.is_floating_point()):
-        raise MTError(-1, where, "counter_dev is one 64-bit integer")
-    _check(lib().mt_kernel_dropout(x_ptr, r_ptr, y_ptr, rows, cols, x_stride, r_stride, y_stride, x_dtype, y_dtype, p,
-                                   seed & 0xFFFFFFFFFFFFFFFF, counter & 0xFFFFFFFFFFFFFFFF, _ptr(counter_dev), _stream_of(device, stream)), where)
-
-
-def _bf16_matrix(where: str, t, rows: int, cols: int):
-    pointer, dtype, stride = _matrix(where, t, rows, cols)
-    if dtype != DTYPE_BF16:
-        raise MTError(-7, where, f"dtype {t.dtype}")
-    # (nobody walks the stride of a single row: any that the library takes will do)
-    return pointer, stride if rows > 1 else cols
+    if counter_dev is not None:
+        if counter_dev.get_device() != device:
+            raise _elsewhere(where, counter_dev, device)
+        if counter_dev.numel() != 1 or counter_dev.element_size() != 8 or counter_dev.is_floating_point():
+            raise MTError(-1, where, "counter_dev is one 64-bit integer")
+        c_ptr = counter_dev.data_ptr()
+    code = lib().mt_kernel_dropout(x_ptr, r_ptr, y_ptr, rows, cols, x_stride, r_stride, y_stride, x_dtype, y_dtype, p,
+                                   seed & 0xFFFFFFFFFFFFFFFF, counter & 0xFFFFFFFFFFFFFFFF, c_ptr, stream)
+    _check(code, where)
 
 
 def mt_kernel_vocab_loss_workspace(rows: int, vocab: int, hidden: int) -> int:
@@ -360,14 +397,16 @@ def mt_kernel_vocab_loss_workspace(rows: int, vocab: int, hidden: int) -> int:
 def mt_kernel_vocab_loss(x, w, bias, labels, loss, lse, workspace, status=None, stream=None) -> None:
     """loss[n] = lse[n] - z[n, labels[n]], lse = log sum exp z, z = x w^T + bias; both 0 where labels[n] < 0."""
     where = "mt_kernel_vocab_loss"
-    device = _operands(where, x, w, bias, labels, loss, lse, workspace, status)
+    torch, device, stream = _begin(where, stream)
     (rows, hidden), vocab = x.shape, w.shape[0]
-    x_ptr, x_stride = _bf16_matrix(where, x, rows, hidden)
-    w_ptr, w_stride = _bf16_matrix(where, w, vocab, hidden)
-    _check(lib().mt_kernel_vocab_loss(x_ptr, w_ptr, _vector(where, bias, vocab, "bfloat16"), _vector(where, labels, rows, "int32"),
-                                      _vector(where, loss, rows, "float32"), _vector(where, lse, rows, "float32"), rows, vocab, hidden,
-                                      x_stride, w_stride, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(status),
-                                      _stream_of(device, stream)), where)
+    x_ptr, x_stride = _bf16_matrix(where, device, x, rows, hidden)
+    w_ptr, w_stride = _bf16_matrix(where, device, w, vocab, hidden)
+    ws_ptr, ws_bytes = _memory(where, device, workspace)
+    code = lib().mt_kernel_vocab_loss(x_ptr, w_ptr, _vector(where, device, bias, vocab, torch.bf16),
+                                      _vector(where, device, labels, rows, torch.i32), _vector(where, device, loss, rows, torch.f32),
+                                      _vector(where, device, lse, rows, torch.f32), rows, vocab, hidden, x_stride, w_stride, ws_ptr,
+                                      ws_bytes, _status_word(where, device, status), stream)
+    _check(code, where)
 
 
 def mt_kernel_vocab_loss_grad_workspace(rows: int, vocab: int, hidden: int) -> int:
@@ -379,17 +418,20 @@ def mt_kernel_vocab_loss_grad(x, w, bias, labels, lse, grad_loss, grad_x, grad_w
     """Gradients of (grad_loss * loss).sum(); grad_loss None stands for ones, a gradient that is None is not taken.  ``accumulate``
     adds to grad_w and grad_bias."""
     where = "mt_kernel_vocab_loss_grad"
-    device = _operands(where, x, w, bias, labels, lse, grad_loss, grad_x, grad_w, grad_bias, workspace, status)
+    torch, device, stream = _begin(where, stream)
     (rows, hidden), vocab = x.shape, w.shape[0]
-    x_ptr, x_stride = _bf16_matrix(where, x, rows, hidden)
-    w_ptr, w_stride = _bf16_matrix(where, w, vocab, hidden)
-    dx_ptr, dx_stride = _bf16_matrix(where, grad_x, rows, hidden) if grad_x is not None else (0, hidden)
-    dw_ptr, dw_stride = _bf16_matrix(where, grad_w, vocab, hidden) if grad_w is not None else (0, hidden)
-    _check(lib().mt_kernel_vocab_loss_grad(x_ptr, w_ptr, _vector(where, bias, vocab, "bfloat16"), _vector(where, labels, rows, "int32"),
-                                           _vector(where, lse, rows, "float32"), _vector(where, grad_loss, rows, "float32"), dx_ptr, dw_ptr,
-                                           _vector(where, grad_bias, vocab, "float32"), rows, vocab, hidden, x_stride, w_stride, dx_stride,
-                                           dw_stride, 1 if accumulate else 0, workspace.data_ptr(),
-                                           workspace.numel() * workspace.element_size(), _ptr(status), _stream_of(device, stream)), where)
+    x_ptr, x_stride = _bf16_matrix(where, device, x, rows, hidden)
+    w_ptr, w_stride = _bf16_matrix(where, device, w, vocab, hidden)
+    dx_ptr, dx_stride = _bf16_matrix(where, device, grad_x, rows, hidden) if grad_x is not None else (0, hidden)
+    dw_ptr, dw_stride = _bf16_matrix(where, device, grad_w, vocab, hidden) if grad_w is not None else (0, hidden)
+    ws_ptr, ws_bytes = _memory(where, device, workspace)
+    code = lib().mt_kernel_vocab_loss_grad(x_ptr, w_ptr, _vector(where, device, bias, vocab, torch.bf16),
+                                           _vector(where, device, labels, rows, torch.i32), _vector(where, device, lse, rows, torch.f32),
+                                           _vector(where, device, grad_loss, rows, torch.f32), dx_ptr, dw_ptr,
+                                           _vector(where, device, grad_bias, vocab, torch.f32), rows, vocab, hidden, x_stride, w_stride,
+                                           dx_stride, dw_stride, 1 if accumulate else 0, ws_ptr, ws_bytes,
+                                           _status_word(where, device, status), stream)
+    _check(code, where)
 
 
 # ---------------------------------------------------------------------------

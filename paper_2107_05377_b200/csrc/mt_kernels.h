@@ -473,9 +473,9 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
 cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStream_t stream);
 
 // The products.  Index 1 of the maps of x: the rows with a label, gathered.  Boxes of 128 x 64 (block_n / 2 x 64) for operands along K,
-// 64 x 64 for operands whose rows run along K, 32 rows x 128 bytes for results.
+// 64 x 64 for operands whose rows run along K.
 struct VocabLossParams {
-  CUtensorMap x_k[2], w_k, x_mn[2], w_mn, g_k, g_mn, g_out, dx_out, dw_out;
+  CUtensorMap x_k[2], w_k, x_mn[2], w_mn, g_k, g_mn;
   const bf16* bias;
   const int32_t* labels;       // of the rows in use
   const int32_t* count;        // rows in use (or null: rows)
@@ -484,6 +484,8 @@ struct VocabLossParams {
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
   float2* parts;
   float* bias_parts;           // backward: sums of g over 32 rows each, [block][bias_pitch]; or null
+  bf16* g;                     // two buffers of row_pitch rows, g_pitch columns each
+  float* dx_sums;              // [ranges][row_pitch][hidden]
   bf16* dw;
   int64_t dw_stride;
   uint32_t* counter;           // next tile to hand out
@@ -495,7 +497,7 @@ struct VocabLossParams {
   int32_t row_pitch;           // rows in whole tiles
   int32_t ranges;              // of the vocabulary, for dx
   int32_t prev_first;          // dx is stored, not added to
-  int32_t part_pitch, bias_pitch;
+  int32_t part_pitch, bias_pitch, g_pitch;
   int32_t want_x, want_w, accumulate;
 };
 struct VocabRowsParams {

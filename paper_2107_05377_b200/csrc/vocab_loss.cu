@@ -18,7 +18,7 @@
 // so neither g nor any input is ever transposed in memory.  Rows without a label take no part: where there are some, the rows that have
 // one are gathered first (their places stay on the device; the grids are sized for all rows and bound their tiles by the count).
 //
-// dx is a sum over all pieces: kept in fp32 in the workspace, added to by TMA reductions (one tile per element and launch, so the
+// dx is a sum over all pieces: kept in fp32 in the workspace, added to by reductions in L2 (one tile per element and launch, so the
 // order is that of the launches), where a launch has few tiles of it in several ranges of the vocabulary with a place each; a last
 // kernel adds the ranges in order and rounds once.
 //
@@ -37,7 +37,7 @@ constexpr int kStageA = kHalf * 128;       // bytes: 128 rows of 64 elements, or
 constexpr int kStageB = kHalf * 128;
 constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 32 * (2 + kEpilogueWarps);
-constexpr int kStaging = 4096;             // of an epilogue warp: 32 rows of 128 bytes
+constexpr int kGroups = kEpilogueWarps / 4;   // epilogue warps of the same rows, which share the columns of a tile
 constexpr int kBook = 1024;
 constexpr int kSlots = 4;                  // tiles announced ahead
 constexpr uint32_t kTmemCols = 512;
@@ -45,10 +45,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -1e30f;           // below every logit that counts; finite, so that -inf minus it is no NaN
 
-__host__ __device__ constexpr int stages(bool grad) { return grad ? 6 : 7; }
-__host__ __device__ constexpr int smem_bytes(bool grad) {
-  return stages(grad) * (kStageA + kStageB) + (grad ? kEpilogueWarps * kStaging : 0) + kBook + 1024;
-}
+// All of shared memory is the ring: what a pair computes is bound by how many bytes are on their way (32 KB per k-block and CTA, of the 64
+// per clock that an SM takes in), so results leave straight from registers instead of through staging buffers.  (Forward, 8192 rows x
+// 30522 x 1024: 282 us, 1.8 PFLOP/s in isolation; g of 3840 columns of it: 45 us.)
+constexpr int kStages = 7;
+constexpr int kSmemBytes = kStages * (kStageA + kStageB) + kBook + 1024;
 
 // Shared-memory descriptor of a tile whose 128-byte rows (64 elements of M or N, 128-byte swizzle) run along K: eight of them make an
 // atom, the next eight along K follow 1024 bytes on, the next 64 elements of M or N 8192 bytes on (boxes of 64 rows).
@@ -62,14 +63,39 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t smem_addr) {
 }
 constexpr uint32_t kAlongMnA = 1u << 15, kAlongMnB = 1u << 16;   // instruction descriptor: the operand's rows run along K
 
-// Shared -> global addition of an fp32 tile; what lies outside the tensor is clipped.
-__device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
-  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];"
-               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y)
-               : "memory");
+// Four lanes that hold four 16-byte pieces of a row each: afterwards piece i of a lane is piece (lane & 3) of the row of the i-th of them,
+// so that a store covers 64 bytes of eight rows instead of 16 bytes of thirty-two.
+__device__ __forceinline__ void exchange_pieces(uint4 (&v)[4], int lane) {
+#pragma unroll
+  for (int k = 1; k <= 2; k <<= 1) {
+    const bool upper = (lane & k) != 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i & k) continue;
+      uint4 give = upper ? v[i] : v[i | k];
+      give.x = __shfl_xor_sync(0xffffffffu, give.x, k);
+      give.y = __shfl_xor_sync(0xffffffffu, give.y, k);
+      give.z = __shfl_xor_sync(0xffffffffu, give.z, k);
+      give.w = __shfl_xor_sync(0xffffffffu, give.w, k);
+      if (upper) v[i] = give; else v[i | k] = give;
+    }
+  }
 }
-__device__ __forceinline__ void st_cluster_u32(uint32_t cluster_addr, uint32_t v) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+__device__ __forceinline__ void red_add_v4(float* p, const uint4& v) {
+  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)),
+               "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)) : "memory");
+}
+// An arrival on a barrier of either CTA of the pair, ordered behind this thread's own accesses in shared and tensor memory only.  (Released
+// at cluster scope it would wait for the thread's stores to global memory as well: some 2000 clocks per tile.)
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// A word into the shared memory of a CTA of the pair, counted on a barrier there that this announces it to: whoever waits for the barrier
+// sees the word, without fences at cluster scope on either side.
+__device__ __forceinline__ void send_word(uint32_t cluster_addr, uint32_t v, uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 4;" ::"r"(cluster_bar) : "memory");
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(cluster_addr), "r"(v), "r"(cluster_bar)
+               : "memory");
 }
 
 // The tiles of a launch, in the order in which they are handed out: long ones first.
@@ -180,13 +206,12 @@ __device__ __forceinline__ float column_sums(float (&c)[32], int lane) {
 
 template <bool GRAD>
 __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
-  constexpr int STAGES = stages(GRAD);
+  constexpr int STAGES = kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sA = smem_u32(smem);
   const uint32_t sB = sA + STAGES * kStageA;
-  const uint32_t sStage = sB + STAGES * kStageB;
-  uint8_t* book = smem + STAGES * (kStageA + kStageB) + (GRAD ? kEpilogueWarps * kStaging : 0);
+  uint8_t* book = smem + STAGES * (kStageA + kStageB);
   const uint32_t bar_full = smem_u32(book);
   const uint32_t bar_empty = bar_full + 8 * STAGES;
   const uint32_t bar_acc_full = bar_empty + 8 * STAGES;
@@ -232,6 +257,9 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
     prefetch_tensormap(&p.x_k[0]);
     prefetch_tensormap(&p.w_k);
   }
+  // (a first look at each line of the arguments costs some hundred clocks: before the wait, not after)
+  asm volatile("" ::"r"(p.rows), "r"(p.cols), "r"(p.block_n), "r"(p.block_h), "r"(p.prev_cols), "r"(p.row_pitch), "r"(p.ranges), "r"(p.want_w),
+               "l"(p.labels), "l"(p.counter));
   grid_dependency_wait();
   grid_launch_dependents();
   const int rows = p.count != nullptr ? min(p.rows, *reinterpret_cast<const volatile int*>(p.count)) : p.rows;
@@ -246,10 +274,10 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
   uint32_t slot_phase = 0;
   // the roles other than rank 0's producer: the next tile, or -1 at the end and when the CTA is giving up
   auto next_announced = [&]() -> int {
-    if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_slot_full + 8 * slot, slot_phase, abort_flag))) return -1;
+    if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_full + 8 * slot, slot_phase, abort_flag))) return -1;
     const int i = static_cast<int>(slot_tile[slot]);
     __syncwarp();
-    if (lane == 0) mbar_arrive_cluster(bar_slot_empty_0 + 8 * slot);
+    if (lane == 0) mbar_arrive_remote(bar_slot_empty_0 + 8 * slot);
     if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
     return i < total ? i : -1;
   };
@@ -261,7 +289,23 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
     uint32_t phase = 0;
     long long issued = 0;
     bool ok = true;
-    int taken = worker;                            // (static: the tile; dynamic, rank 0: asked for one tile ahead)
+    int taken = worker;
+    // (backward, rank 0) Tile `i` of the list to the other roles; the tile after the one whose copies are under way is asked for when its
+    // turn begins and announced some k-blocks later, so that neither the trip to the counter nor that to the other CTA holds up a copy.
+    int asked = 0;
+    auto announce = [&](int i) -> bool {
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) return false;
+      if (lane < 2)
+        send_word(map_to_cta(smem_u32(const_cast<uint32_t*>(slot_tile) + slot), lane), static_cast<uint32_t>(i),
+                  map_to_cta(bar_slot_full + 8 * slot, lane));
+      __syncwarp();
+      if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
+      return true;
+    };
+    if (GRAD && rank == 0) {
+      ok = announce(taken);
+      if (lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
+    }
     for (bool begun = false; ok; begun = true) {
       int i;
       if (!GRAD) {
@@ -270,17 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
       } else if (rank != 0) {
         i = next_announced();
       } else {
-        if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) { ok = false; break; }
-        i = __shfl_sync(0xffffffffu, taken, 0);
-        if (lane == 0) {
-          for (uint32_t r = 0; r < 2; ++r) {
-            st_cluster_u32(map_to_cta(smem_u32(const_cast<uint32_t*>(slot_tile) + slot), r), static_cast<uint32_t>(i));
-            mbar_arrive_cluster(map_to_cta(bar_slot_full + 8 * slot, r));
-          }
-        }
-        if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
-        if (i >= total) i = -1;
-        else if (lane == 0) taken = n_workers + static_cast<int>(atomicAdd(p.counter, 1u));   // the one after this
+        i = taken < total ? taken : -1;
       }
       if (i < 0) break;
       const Tile t = find_tile<GRAD>(p, work, i);
@@ -310,6 +344,16 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
         }
         ++issued;
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        if (GRAD && rank == 0 && kb == min(3, t.k_blocks - 1)) {
+          taken = n_workers + __shfl_sync(0xffffffffu, asked, 0);
+          if (!announce(taken)) { ok = false; break; }
+          if (lane == 0 && taken < total) asked = static_cast<int>(atomicAdd(p.counter, 1u));
+        }
+      }
+      if (GRAD && rank == 0 && ok && t.k_blocks == 0) {
+        taken = n_workers + __shfl_sync(0xffffffffu, asked, 0);
+        ok = announce(taken);
+        if (ok && lane == 0 && taken < total) asked = static_cast<int>(atomicAdd(p.counter, 1u));
       }
     }
     if (!ok && rank == 0 && leader) {
@@ -367,9 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
     // ------------------------------ epilogue ----------------------------------
     const int e = warp - 2;
     const int quarter = warp & 3;
-    const int group = e >> 2;                           // of the two that share the chunks of columns
-    const uint32_t my_stage = sStage + static_cast<uint32_t>(e * kStaging);
-    uint8_t* my_stage_ptr = smem + STAGES * (kStageA + kStageB) + e * kStaging;
+    const int group = e >> 2;
     const uint32_t bar_acc_empty_0 = map_to_cta(bar_acc_empty, 0);
     int acc = 0;
     uint32_t acc_phase = 0;
@@ -403,9 +445,9 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
         float top2 = kFloor, sum = 0.f;                 // largest logit times log2 e, sum of 2^(z log2 e - top2)
         const int n0 = t.n * p.block_n;
 #pragma unroll 1
-        for (int c = group * 32; c < p.block_n; c += 64) {
+        for (int c = group * 32; c < p.block_n; c += 32 * kGroups) {
           const int col = n0 + c;
-          if (col >= p.vocab) break;
+          if (col >= p.vocab || m0 >= rows) break;
           uint32_t v[32];
           tmem_ld_32x32(taddr0 + c, v);
           tmem_ld_wait();
@@ -435,64 +477,56 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
           for (int j = 0; j < 32; ++j) s[j & 3] += ex2_approx(fmaf(z[j], kLog2e, -top2));
           sum += (s[0] + s[1]) + (s[2] + s[3]);
         }
-        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + 2 * t.n + group] = make_float2(top2, sum);
+        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + kGroups * t.n + group] = make_float2(top2, sum);
       } else if (t.kind == 0) {
         const int n0 = t.n * p.block_n;                 // in the piece
         const bool whole = __all_sync(0xffffffffu, row_counts);
+        bf16* g_out = p.g + static_cast<int64_t>(p.g_row0 + m0 + (lane & ~3)) * p.g_pitch + (lane & 3) * 8;
 #pragma unroll 1
-        for (int c = group * 64; c < p.block_n; c += 128) {
-          if (n0 + c >= p.cols) break;
-          // the store that last read this buffer must be done with it
-          if (lane == 0) tma_store_wait_read<0>();
-          __syncwarp();
+        for (int c = group * 32; c < p.block_n; c += 32 * kGroups) {
+          const int local = n0 + c;
+          if (local >= p.cols || m0 >= work.row_k * 64) break;   // (kind 2 sums over rows in whole k-blocks)
+          const int col = p.col0 + local;
+          uint32_t v[32];
+          tmem_ld_32x32(taddr0 + c, v);
+          tmem_ld_wait();
+          float g[32];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int local = n0 + c + half * 32;
-            const int col = p.col0 + local;
-            uint32_t v[32];
-            tmem_ld_32x32(taddr0 + c + half * 32, v);
-            tmem_ld_wait();
-            float g[32];
+          for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(v[j]);
+          add_bias(p.bias, col, p.vocab, g);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(v[j]);
-            add_bias(p.bias, col, p.vocab, g);
+          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, minus_lse2));
+          const int at = label - col;
+          if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, minus_lse2));
-            const int at = label - col;
-            if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) if (j == at) g[j] -= 1.f;
-            }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] *= weight;
-            if (!whole) {                               // (behind the last row lies anything)
-#pragma unroll
-              for (int j = 0; j < 32; ++j) g[j] = row_counts ? g[j] : 0.f;
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              *reinterpret_cast<uint4*>(my_stage_ptr + staging_off(lane, half * 4 + q)) =
-                  make_uint4(pack_bf16(g[q * 8], g[q * 8 + 1]), pack_bf16(g[q * 8 + 2], g[q * 8 + 3]), pack_bf16(g[q * 8 + 4], g[q * 8 + 5]),
-                             pack_bf16(g[q * 8 + 6], g[q * 8 + 7]));
-            if (p.bias_parts != nullptr && m0 < rows) {
-              const float s = column_sums(g, lane);
-              if (local + lane < p.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + local + lane] = s;
-            }
+            for (int j = 0; j < 32; ++j) if (j == at) g[j] -= 1.f;
           }
-          fence_async_shared();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_2d(&p.g_out, my_stage, n0 + c, p.g_row0 + m0);
-            tma_store_commit();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) g[j] *= weight;
+          if (!whole) {                                 // (behind the last row lies anything)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = row_counts ? g[j] : 0.f;
+          }
+          uint4 out[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            out[q] = make_uint4(pack_bf16(g[q * 8], g[q * 8 + 1]), pack_bf16(g[q * 8 + 2], g[q * 8 + 3]), pack_bf16(g[q * 8 + 4], g[q * 8 + 5]),
+                                pack_bf16(g[q * 8 + 6], g[q * 8 + 7]));
+          exchange_pieces(out, lane);
+          // (columns behind the piece's last are written, up to its pitch, and never read)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(q) * p.g_pitch + local) = out[q];
+          if (p.bias_parts != nullptr && m0 < rows) {
+            const float s = column_sums(g, lane);
+            if (local + lane < p.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + col + lane] = s;
           }
         }
       } else if (t.kind == 1) {
         const int n0 = t.n * p.block_h;
+        float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * p.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
 #pragma unroll 1
-        for (int c = group * 32; c < p.block_h; c += 64) {
+        for (int c = group * 32; c < p.block_h; c += 32 * kGroups) {
           if (n0 + c >= p.hidden || m0 >= rows) break;
-          if (lane == 0) tma_store_wait_read<0>();
-          __syncwarp();
           uint32_t v[32];
           if (t.k_blocks > 0) {
             tmem_ld_32x32(taddr0 + c, v);
@@ -502,72 +536,73 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
             for (int j = 0; j < 32; ++j) v[j] = 0u;
           }
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
-            *reinterpret_cast<uint4*>(my_stage_ptr + staging_off(lane, q)) = make_uint4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-          fence_async_shared();
-          __syncwarp();
-          if (lane == 0) {
-            if (p.prev_first) tma_store_2d(&p.dx_out, my_stage, n0 + c, t.range * p.row_pitch + m0);
-            else tma_add_2d(&p.dx_out, my_stage, n0 + c, t.range * p.row_pitch + m0);
-            tma_store_commit();
+          for (int half = 0; half < 2; ++half) {
+            uint4 out[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              out[q] = make_uint4(v[half * 16 + q * 4], v[half * 16 + q * 4 + 1], v[half * 16 + q * 4 + 2], v[half * 16 + q * 4 + 3]);
+            exchange_pieces(out, lane);
+            const int col = n0 + c + half * 16;
+            if (col + (lane & 3) * 4 >= p.hidden) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float* to = sums + static_cast<int64_t>(q) * p.hidden + col;
+              if (p.prev_first) *reinterpret_cast<uint4*>(to) = out[q]; else red_add_v4(to, out[q]);
+            }
           }
         }
       } else {
         const int n0 = t.n * p.block_h;
-        const int word = p.prev_col0 + row;             // row of dW
+        const int word = p.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
+        bf16* dw = p.dw + static_cast<int64_t>(word) * p.dw_stride + (lane & 3) * 8;
 #pragma unroll 1
-        for (int c = group * 64; c < p.block_h; c += 128) {
-          if (n0 + c >= p.hidden || p.prev_col0 + m0 >= p.vocab) break;
-          if (lane == 0) tma_store_wait_read<0>();
-          __syncwarp();
+        for (int c = group * 32; c < p.block_h; c += 32 * kGroups) {
+          const int col = n0 + c;
+          if (col >= p.hidden || p.prev_col0 + m0 >= p.vocab) break;
+          uint32_t v[32];
+          if (t.k_blocks > 0) {
+            tmem_ld_32x32(taddr0 + c, v);
+            tmem_ld_wait();
+          } else {
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int col = n0 + c + half * 32;
-            uint32_t v[32];
-            if (t.k_blocks > 0) {
-              tmem_ld_32x32(taddr0 + c + half * 32, v);
-              tmem_ld_wait();
-            } else {
+            for (int j = 0; j < 32; ++j) v[j] = 0u;
+          }
+          if (p.accumulate) {
+            const int mine = p.prev_col0 + row;
+            const bf16* old = p.dw + static_cast<int64_t>(mine) * p.dw_stride + col;
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v[j] = 0u;
-            }
-            if (p.accumulate) {
-              const bf16* old = p.dw + static_cast<int64_t>(word) * p.dw_stride + col;
+            for (int q = 0; q < 4; ++q) {               // (hidden is a multiple of eight)
+              if (mine >= p.vocab || col + q * 8 >= p.hidden) continue;
+              const uint4 b = *reinterpret_cast<const uint4*>(old + q * 8);
+              const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {             // (hidden is a multiple of eight)
-                if (word >= p.vocab || col + q * 8 >= p.hidden) continue;
-                const uint4 b = *reinterpret_cast<const uint4*>(old + q * 8);
-                const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  v[q * 8 + 2 * j] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j]) + bf16_lo(w[j]));
-                  v[q * 8 + 2 * j + 1] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j + 1]) + bf16_hi(w[j]));
-                }
+              for (int j = 0; j < 4; ++j) {
+                v[q * 8 + 2 * j] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j]) + bf16_lo(w[j]));
+                v[q * 8 + 2 * j + 1] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j + 1]) + bf16_hi(w[j]));
               }
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              uint32_t o[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) o[j] = pack_bf16(__uint_as_float(v[q * 8 + 2 * j]), __uint_as_float(v[q * 8 + 2 * j + 1]));
-              *reinterpret_cast<uint4*>(my_stage_ptr + staging_off(lane, half * 4 + q)) = make_uint4(o[0], o[1], o[2], o[3]);
-            }
+            __syncwarp();                               // (all of the warp has read before any of it writes)
           }
-          fence_async_shared();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_2d(&p.dw_out, my_stage, n0 + c, p.prev_col0 + m0);
-            tma_store_commit();
+          uint4 out[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = pack_bf16(__uint_as_float(v[q * 8 + 2 * j]), __uint_as_float(v[q * 8 + 2 * j + 1]));
+            out[q] = make_uint4(o[0], o[1], o[2], o[3]);
           }
+          exchange_pieces(out, lane);
+          if (col + (lane & 3) * 8 >= p.hidden) continue;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (word + q < p.vocab) *reinterpret_cast<uint4*>(dw + static_cast<int64_t>(q) * p.dw_stride + col) = out[q];
         }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(bar_acc_empty_0 + 8 * acc);
+      if (lane == 0) mbar_arrive_remote(bar_acc_empty_0 + 8 * acc);
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
-    if (lane == 0) tma_store_wait_read<0>();
-    __syncwarp();
   }
 
   tc_fence_before();
@@ -712,33 +747,35 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __g
   }
 }
 
-// dx: the ranges of a row added up in order, rounded once, to the row's place; zeros for rows without a label.  A warp per row.
+// dx: the ranges of a row added up in order, rounded once, to the row's place; zeros for rows without a label.  A warp per row and 256
+// columns.
 __global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_constant__ VocabDxParams p) {
   grid_dependency_wait();
   grid_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const int step = gridDim.x * (kJoinThreads / 32);
-  for (int row = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); row < p.rows; row += step) {
+  const int blocks = (p.hidden + 255) / 256;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * (kJoinThreads / 32), units = static_cast<int64_t>(p.rows) * blocks;
+  for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); u < units; u += step) {
+    const int row = static_cast<int>(u / blocks), c = static_cast<int>(u % blocks) * 256 + lane * 8;
+    if (c >= p.hidden) continue;
     const int place = p.place_of[row];
-    bf16* out = p.dx + static_cast<int64_t>(row) * p.dx_stride;
-    for (int c = lane * 8; c < p.hidden; c += 256) {
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-      if (place >= 0) {
-        const float* src = p.sums + static_cast<int64_t>(place) * p.hidden + c;
-#pragma unroll 4
-        for (int s = 0; s < p.ranges; ++s) {
-          const float4* f = reinterpret_cast<const float4*>(src + static_cast<int64_t>(s) * p.row_pitch * p.hidden);
-          const float4 u = f[0], w = f[1];
-          a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
-          b.x += w.x; b.y += w.y; b.z += w.z; b.w += w.w;
-        }
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    if (place >= 0) {
+      const float* src = p.sums + static_cast<int64_t>(place) * p.hidden + c;
+#pragma unroll 8
+      for (int s = 0; s < p.ranges; ++s) {
+        const float4* f = reinterpret_cast<const float4*>(src + static_cast<int64_t>(s) * p.row_pitch * p.hidden);
+        const float4 x = f[0], w = f[1];
+        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+        b.x += w.x; b.y += w.y; b.z += w.z; b.w += w.w;
       }
-      *reinterpret_cast<uint4*>(out + c) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
     }
+    *reinterpret_cast<uint4*>(p.dx + static_cast<int64_t>(row) * p.dx_stride + c) =
+        make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
   }
 }
 
-// db of a piece: the sums of all blocks of 32 rows, in order.  A CTA per 32 columns; every warp takes each eighth block.
+// db: the sums of all blocks of 32 rows, in order.  A CTA per 32 columns; every warp takes each eighth block.
 __global__ void __launch_bounds__(256) vocab_bias_kernel(const __grid_constant__ VocabBiasParams p) {
   __shared__ float s_sum[8][32];
   grid_dependency_wait();
@@ -764,12 +801,12 @@ cudaError_t launch_pairs(const VocabLossParams& p, int tiles, int sm_count, cuda
   auto kernel = vocab_loss_pair_tcgen05<GRAD>;
   static PerDeviceOnce once;
   cudaError_t err = per_device_once(once, [&](int) {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes(GRAD));
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   });
   if (err != cudaSuccess) return err;
   const int most = sm_count / 2 > 0 ? sm_count / 2 : 1;
   const int workers = tiles < most ? (tiles > 0 ? tiles : 1) : most;
-  return launch_kernel(kernel, dim3(2 * workers), dim3(kThreads), smem_bytes(GRAD), stream, p, 2u);
+  return launch_kernel(kernel, dim3(2 * workers), dim3(kThreads), kSmemBytes, stream, p, 2u);
 }
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
@@ -804,14 +841,14 @@ ForwardPlan forward_plan(int rows, int vocab, int hidden, int sm_count) {
     if (best < 0 || cost < best) { best = cost; f.block_n = bn; }
   }
   f.tiles_n = ceil_div(vocab, f.block_n);
-  f.part_pitch = 2 * f.tiles_n;
+  f.part_pitch = kGroups * f.tiles_n;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += whole_lines(bytes); return here; };
   f.count = take(256);
   f.row_of = take(f.row_pitch * 4);
   f.row_label = take(f.row_pitch * 4);
   f.label_logit = take(f.row_pitch * 4);
-  f.parts = take(static_cast<size_t>(f.row_pitch) * ceil_div(vocab, kHalf) * 2 * sizeof(float2));   // (for the narrowest tiles)
+  f.parts = take(static_cast<size_t>(f.row_pitch) * ceil_div(vocab, kHalf) * kGroups * sizeof(float2));   // (for the narrowest tiles)
   f.gathered = take(f.gather ? static_cast<size_t>(f.row_pitch) * hidden * 2 : 0);
   f.bytes = at;
   return f;
@@ -856,7 +893,7 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
   f.g = take(static_cast<size_t>(f.buffers) * f.row_pitch * f.piece * 2);
   f.dx = take(static_cast<size_t>(f.ranges) * f.row_pitch * hidden * 4);
-  f.bias_parts = take(static_cast<size_t>(f.row_pitch / 32) * f.piece * 4);
+  f.bias_parts = take(static_cast<size_t>(f.row_pitch / 32) * vocab * 4);
   f.bytes = at;
   return f;
 }
@@ -932,7 +969,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.status = c.status;
   p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate;
   p.dw = c.dw; p.dw_stride = c.dw_stride;
-  p.bias_parts = c.db != nullptr ? at<float>(ws, f.bias_parts) : nullptr; p.bias_pitch = f.piece;
+  p.bias_parts = c.db != nullptr ? at<float>(ws, f.bias_parts) : nullptr; p.bias_pitch = c.vocab;
   bf16* gathered = at<bf16>(ws, f.gathered);
   bf16* g = at<bf16>(ws, f.g);
   const int64_t g_rows = f.buffers * f.row_pitch, g_stride = static_cast<int64_t>(f.piece) * 2, h_stride = static_cast<int64_t>(c.hidden) * 2;
@@ -941,10 +978,9 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
       (e = encode_matrix_map(&p.x_mn[0], c.x, c.rows, c.hidden, c.x_stride * 2, 64, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_mn[1], gathered, f.row_pitch, c.hidden, h_stride, 64, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, kHalf, 64, false)) != cudaSuccess ||
-      (e = encode_matrix_map(&p.w_mn, c.w, c.vocab, c.hidden, c.w_stride * 2, 64, 64, false)) != cudaSuccess ||
-      (e = encode_matrix_map(&p.dx_out, at<float>(ws, f.dx), f.ranges * f.row_pitch, c.hidden, static_cast<int64_t>(c.hidden) * 4, 32, 32, true)) != cudaSuccess)
+      (e = encode_matrix_map(&p.w_mn, c.w, c.vocab, c.hidden, c.w_stride * 2, 64, 64, false)) != cudaSuccess)
     return e;
-  if (c.dw != nullptr && (e = encode_matrix_map(&p.dw_out, c.dw, c.vocab, c.hidden, c.dw_stride * 2, 32, 64, false)) != cudaSuccess) return e;
+  p.g = g; p.g_pitch = f.piece; p.dx_sums = at<float>(ws, f.dx);
   const bool products = c.dx != nullptr || c.dw != nullptr;
   const int row_tiles = static_cast<int>(f.row_pitch / kTile), hidden_tiles = ceil_div(c.hidden, f.block_h);
   for (int j = 0; j <= f.pieces; ++j) {
@@ -958,27 +994,26 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     p.prev_first = j == 1 ? 1 : 0;
     p.counter = r.counters + j;
     // (columns behind the piece's last one are neither stored nor read: the products over the vocabulary see zeros there)
-    if (p.cols > 0 && (e = encode_matrix_map(&p.g_out, g, g_rows, p.cols, g_stride, 32, 64, false)) != cudaSuccess) return e;
     if (p.prev_cols > 0 && ((e = encode_matrix_map(&p.g_k, g, g_rows, p.prev_cols, g_stride, kHalf, 64, false)) != cudaSuccess ||
                             (e = encode_matrix_map(&p.g_mn, g, g_rows, p.prev_cols, g_stride, 64, 64, false)) != cudaSuccess))
       return e;
     const int64_t tiles = static_cast<int64_t>(row_tiles) * ceil_div(p.cols, kTile) +
                           (p.prev_cols > 0 ? static_cast<int64_t>(row_tiles) * hidden_tiles * f.ranges + static_cast<int64_t>(ceil_div(p.prev_cols, kTile)) * hidden_tiles : 0);
     if ((e = launch_pairs<true>(p, static_cast<int>(tiles < (1 << 30) ? tiles : 1 << 30), sm_count, stream)) != cudaSuccess) return e;
-    if (c.db != nullptr && j < f.pieces) {
-      VocabBiasParams b;
-      memset(&b, 0, sizeof(b));
-      b.parts = p.bias_parts; b.pitch = f.piece; b.count = r.count; b.rows = c.rows; b.cols = p.cols; b.out = c.db + p.col0; b.accumulate = c.accumulate;
-      if ((e = launch_kernel(vocab_bias_kernel, dim3(ceil_div(p.cols, 32)), dim3(256), 0, stream, b)) != cudaSuccess) return e;
-    }
+  }
+  if (c.db != nullptr) {
+    VocabBiasParams b;
+    memset(&b, 0, sizeof(b));
+    b.parts = p.bias_parts; b.pitch = c.vocab; b.count = r.count; b.rows = c.rows; b.cols = c.vocab; b.out = c.db; b.accumulate = c.accumulate;
+    if ((e = launch_kernel(vocab_bias_kernel, dim3(ceil_div(c.vocab, 32)), dim3(256), 0, stream, b)) != cudaSuccess) return e;
   }
   if (c.dx == nullptr) return cudaSuccess;
   VocabDxParams d;
   memset(&d, 0, sizeof(d));
   d.sums = at<float>(ws, f.dx); d.place_of = r.place_of; d.dx = c.dx; d.dx_stride = c.dx_stride; d.rows = c.rows; d.hidden = c.hidden;
   d.row_pitch = f.row_pitch; d.ranges = f.ranges;
-  const int dx_ctas = ceil_div(c.rows, kJoinThreads / 32);
-  return launch_kernel(vocab_dx_kernel, dim3(dx_ctas < 16 * sm_count ? dx_ctas : 16 * sm_count), dim3(kJoinThreads), 0, stream, d);
+  const int64_t dx_ctas = (static_cast<int64_t>(c.rows) * ceil_div(c.hidden, 256) + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
+  return launch_kernel(vocab_dx_kernel, dim3(static_cast<unsigned>(dx_ctas < 16 * sm_count ? dx_ctas : 16 * sm_count)), dim3(kJoinThreads), 0, stream, d);
 }
 
 }  // namespace mt
