@@ -481,6 +481,7 @@ struct VocabLossParams {
   const int32_t* count;        // rows in use (or null: rows)
   const float* row_lse;
   const float* row_weight;
+  float* row_residual;         // backward: what rounding takes from the label's entry of g
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
   float2* parts;
   float* bias_parts;           // backward: sums of g over 32 rows each, [block][bias_pitch]; or null
@@ -499,6 +500,27 @@ struct VocabLossParams {
   int32_t prev_first;          // dx is stored, not added to
   int32_t part_pitch, bias_pitch, g_pitch;
   int32_t want_x, want_w, accumulate;
+  int32_t by_words;            // g lies by words, [vocab][rows] (few rows; g_k: boxes of 128 words, g_mn: of 64)
+};
+// Up to 128 rows: the logits turned, words on the lanes.
+struct VocabFewParams {
+  CUtensorMap x_k, w_k;        // boxes of all rows (rounded up to 16) x 64 and of 128 x 64
+  const bf16* bias;
+  const int32_t* labels;
+  float* label_logit;          // forward: of every row; and (largest logit, sum) of every CTA, [row][part_pitch]
+  float2* parts;
+  const float* lse;            // backward
+  const float* grad_loss;
+  const bf16* x;
+  int64_t x_stride;
+  bf16* x_clean;               // [g_pitch][hidden], zeros in rows without a label; or null
+  bf16* g;                     // [vocab in whole tiles][g_pitch]
+  float* db;
+  float* row_residual;
+  uint32_t* counter;           // set to zero (for the products)
+  uint32_t* status;
+  int32_t rows, vocab, hidden, part_pitch, g_pitch, accumulate;
+  int32_t columns, stages, stage_bytes;   // chosen by the launcher
 };
 struct VocabRowsParams {
   const int32_t* labels;
@@ -532,10 +554,14 @@ struct VocabJoinParams {
 };
 struct VocabDxParams {
   const float* sums;           // [ranges][row_pitch][hidden]
-  const int32_t* place_of;
+  const int32_t* place_of;     // or null: in place
+  const int32_t* labels;
+  const float* row_residual;
+  const bf16* w;
+  int64_t w_stride;
   bf16* dx;
   int64_t dx_stride, row_pitch;
-  int32_t rows, hidden, ranges;
+  int32_t rows, vocab, hidden, ranges;
 };
 struct VocabBiasParams {
   const float* parts;

@@ -35,9 +35,10 @@ constexpr int kTile = 256;                 // rows and (at most) columns of a pa
 constexpr int kHalf = 128;                 // rows of a CTA
 constexpr int kStageA = kHalf * 128;       // bytes: 128 rows of 64 elements, or two boxes of 64 x 64
 constexpr int kStageB = kHalf * 128;
-constexpr int kEpilogueWarps = 8;
-constexpr int kThreads = 32 * (2 + kEpilogueWarps);
-constexpr int kGroups = kEpilogueWarps / 4;   // epilogue warps of the same rows, which share the columns of a tile
+// Epilogue warps: in the gradient's short tiles (few rows: two k-blocks) they are what a tile takes.
+__host__ __device__ constexpr int epilogue_warps(bool grad) { return grad ? 16 : 8; }
+__host__ __device__ constexpr int threads(bool grad) { return 32 * (2 + epilogue_warps(grad)); }
+__host__ __device__ constexpr int groups(bool grad) { return epilogue_warps(grad) / 4; }   // of the same rows: they share the columns
 constexpr int kBook = 1024;
 constexpr int kSlots = 4;                  // tiles announced ahead
 constexpr uint32_t kTmemCols = 512;
@@ -90,11 +91,12 @@ __device__ __forceinline__ void red_add_v4(float* p, const uint4& v) {
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// A word into the shared memory of a CTA of the pair, counted on a barrier there that this announces it to: whoever waits for the barrier
-// sees the word, without fences at cluster scope on either side.
-__device__ __forceinline__ void send_word(uint32_t cluster_addr, uint32_t v, uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 4;" ::"r"(cluster_bar) : "memory");
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(cluster_addr), "r"(v), "r"(cluster_bar)
+// Four words into the shared memory of a CTA of the pair, counted on a barrier there that this announces them to: whoever waits for the
+// barrier sees them, without fences at cluster scope on either side.
+__device__ __forceinline__ void send_words(uint32_t cluster_addr, int a, int b, int c, int d, uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 16;" ::"r"(cluster_bar) : "memory");
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.s32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(cluster_addr), "r"(a), "r"(b), "r"(c), "r"(d), "r"(cluster_bar)
                : "memory");
 }
 
@@ -205,8 +207,9 @@ __device__ __forceinline__ float column_sums(float (&c)[32], int lane) {
 }
 
 template <bool GRAD>
-__global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
+__global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
   constexpr int STAGES = kStages;
+  constexpr int EPILOGUE_WARPS = epilogue_warps(GRAD), GROUPS = groups(GRAD);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sA = smem_u32(smem);
@@ -218,8 +221,9 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
   const uint32_t bar_acc_empty = bar_acc_full + 16;
   const uint32_t bar_slot_full = bar_acc_empty + 16;
   const uint32_t bar_slot_empty = bar_slot_full + 8 * kSlots;      // (of rank 0)
-  volatile uint32_t* slot_tile = reinterpret_cast<volatile uint32_t*>(book + 8 * (2 * STAGES + 4 + 2 * kSlots));
-  uint32_t* tmem_slot = const_cast<uint32_t*>(slot_tile) + kSlots;
+  static_assert((2 * STAGES + 4 + 2 * kSlots) % 2 == 0, "tiles are sent in 16 bytes");
+  volatile int4* slot_tile = reinterpret_cast<volatile int4*>(book + 8 * (2 * STAGES + 4 + 2 * kSlots));   // kind, m, n + 65536 range, k-blocks
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * STAGES + 4 + 2 * kSlots) + 16 * kSlots);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5;
@@ -235,11 +239,11 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(bar_acc_full + 8 * a, 1);
-      mbar_init(bar_acc_empty + 8 * a, 2 * kEpilogueWarps);
+      mbar_init(bar_acc_empty + 8 * a, 2 * EPILOGUE_WARPS);
     }
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(bar_slot_full + 8 * s, 1);
-      mbar_init(bar_slot_empty + 8 * s, 2 * kEpilogueWarps + 2);   // all epilogue warps, the MMA warp, rank 1's producer
+      mbar_init(bar_slot_empty + 8 * s, 2 * EPILOGUE_WARPS + 2);   // all epilogue warps, the MMA warp, rank 1's producer
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -254,8 +258,16 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
   const uint32_t bar_full_count = map_to_cta(bar_full, 0);
   const uint32_t bar_slot_empty_0 = map_to_cta(bar_slot_empty, 0);
   if (warp == 0 && lane == 0) {
-    prefetch_tensormap(&p.x_k[0]);
-    prefetch_tensormap(&p.w_k);
+    if (!GRAD || p.cols > 0) {
+      prefetch_tensormap(&p.x_k[0]);
+      prefetch_tensormap(&p.w_k);
+    }
+    if (GRAD && p.prev_cols > 0) {
+      prefetch_tensormap(&p.w_mn);
+      prefetch_tensormap(&p.g_k);
+      prefetch_tensormap(&p.g_mn);
+      prefetch_tensormap(&p.x_mn[0]);
+    }
   }
   // (a first look at each line of the arguments costs some hundred clocks: before the wait, not after)
   asm volatile("" ::"r"(p.rows), "r"(p.cols), "r"(p.block_n), "r"(p.block_h), "r"(p.prev_cols), "r"(p.row_pitch), "r"(p.ranges), "r"(p.want_w),
@@ -272,14 +284,36 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
   // has no influence on it.)
   int slot = 0;
   uint32_t slot_phase = 0;
-  // the roles other than rank 0's producer: the next tile, or -1 at the end and when the CTA is giving up
-  auto next_announced = [&]() -> int {
-    if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_full + 8 * slot, slot_phase, abort_flag))) return -1;
-    const int i = static_cast<int>(slot_tile[slot]);
+  // Forward: m and n of the next tile of this worker without a division per tile.
+  const int step_m = n_workers % max(work.row_tiles, 1), step_n = n_workers / max(work.row_tiles, 1);
+  Tile t;
+  t.kind = 0; t.range = 0; t.k_begin = 0; t.k_blocks = work.k0;
+  t.m = worker % max(work.row_tiles, 1);
+  t.n = worker / max(work.row_tiles, 1);
+  int at_tile = worker;
+  auto next_static = [&](bool first) -> bool {
+    if (!first) {
+      at_tile += n_workers;
+      t.m += step_m;
+      t.n += step_n;
+      if (t.m >= work.row_tiles) { t.m -= work.row_tiles; ++t.n; }
+    }
+    return at_tile < total;
+  };
+  // Backward, the roles other than rank 0's producer: the next tile; false at the end and when the CTA is giving up.
+  auto next_announced = [&]() -> bool {
+    if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_full + 8 * slot, slot_phase, abort_flag))) return false;
+    t.kind = slot_tile[slot].x;
+    t.m = slot_tile[slot].y;
+    const int n_range = slot_tile[slot].z;
+    t.k_blocks = slot_tile[slot].w;
+    t.n = n_range & 0xFFFF;
+    t.range = n_range >> 16;
+    t.k_begin = t.range * work.k1;
     __syncwarp();
     if (lane == 0) mbar_arrive_remote(bar_slot_empty_0 + 8 * slot);
     if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
-    return i < total ? i : -1;
+    return t.kind >= 0;
   };
 
   if (warp == 0) {
@@ -289,35 +323,31 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
     uint32_t phase = 0;
     long long issued = 0;
     bool ok = true;
-    int taken = worker;
-    // (backward, rank 0) Tile `i` of the list to the other roles; the tile after the one whose copies are under way is asked for when its
-    // turn begins and announced some k-blocks later, so that neither the trip to the counter nor that to the other CTA holds up a copy.
+    // (backward, rank 0) The tile after the one whose copies are under way is asked for when its turn begins and announced some k-blocks
+    // later, so that neither the trip to the counter nor that to the other CTA holds up a copy.
     int asked = 0;
+    Tile ahead = t;
     auto announce = [&](int i) -> bool {
+      if (i < total) ahead = find_tile<GRAD>(p, work, i); else ahead.kind = -1;
       if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) return false;
       if (lane < 2)
-        send_word(map_to_cta(smem_u32(const_cast<uint32_t*>(slot_tile) + slot), lane), static_cast<uint32_t>(i),
-                  map_to_cta(bar_slot_full + 8 * slot, lane));
+        send_words(map_to_cta(smem_u32(const_cast<int4*>(slot_tile) + slot), lane), ahead.kind, ahead.m, ahead.n | (ahead.range << 16), ahead.k_blocks,
+                   map_to_cta(bar_slot_full + 8 * slot, lane));
       __syncwarp();
       if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
+      if (ahead.kind >= 0 && lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
       return true;
     };
-    if (GRAD && rank == 0) {
-      ok = announce(taken);
-      if (lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
-    }
-    for (bool begun = false; ok; begun = true) {
-      int i;
+    if (GRAD && rank == 0) ok = announce(worker);
+    for (bool first = true; ok; first = false) {
       if (!GRAD) {
-        if (begun) taken += n_workers;
-        i = taken < total ? taken : -1;
+        if (!next_static(first)) break;
       } else if (rank != 0) {
-        i = next_announced();
+        if (!next_announced()) break;
       } else {
-        i = taken < total ? taken : -1;
+        t = ahead;
+        if (t.kind < 0) break;
       }
-      if (i < 0) break;
-      const Tile t = find_tile<GRAD>(p, work, i);
       const int half_n = (t.kind == 0 ? p.block_n : p.block_h) / 2;
       const uint32_t bytes = 2 * (kStageA + half_n * 128);
       const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf;
@@ -332,29 +362,30 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
             tma_load_2d_pair(a, &p.x_k[gathered], k, m0, bar);
             tma_load_2d_pair(b, &p.w_k, k, p.col0 + n0, bar);
           } else if (t.kind == 1) {
-            tma_load_2d_pair(a, &p.g_k, k, p.prev_g_row0 + m0, bar);
+            if (p.by_words) {
+              tma_load_2d_pair(a, &p.g_mn, m0, p.prev_col0 + k, bar);
+              tma_load_2d_pair(a + 8192, &p.g_mn, m0 + 64, p.prev_col0 + k, bar);
+            } else {
+              tma_load_2d_pair(a, &p.g_k, k, p.prev_g_row0 + m0, bar);
+            }
             tma_load_2d_pair(b, &p.w_mn, n0, p.prev_col0 + k, bar);
             if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, p.prev_col0 + k, bar);
           } else {
-            tma_load_2d_pair(a, &p.g_mn, m0, p.prev_g_row0 + k, bar);
-            tma_load_2d_pair(a + 8192, &p.g_mn, m0 + 64, p.prev_g_row0 + k, bar);
+            if (p.by_words) {
+              tma_load_2d_pair(a, &p.g_k, k, p.prev_col0 + m0, bar);
+            } else {
+              tma_load_2d_pair(a, &p.g_mn, m0, p.prev_g_row0 + k, bar);
+              tma_load_2d_pair(a + 8192, &p.g_mn, m0 + 64, p.prev_g_row0 + k, bar);
+            }
             tma_load_2d_pair(b, &p.x_mn[gathered], n0, k, bar);
             if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, k, bar);
           }
         }
         ++issued;
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        if (GRAD && rank == 0 && kb == min(3, t.k_blocks - 1)) {
-          taken = n_workers + __shfl_sync(0xffffffffu, asked, 0);
-          if (!announce(taken)) { ok = false; break; }
-          if (lane == 0 && taken < total) asked = static_cast<int>(atomicAdd(p.counter, 1u));
-        }
+        if (GRAD && rank == 0 && kb == min(3, t.k_blocks - 1) && !announce(n_workers + __shfl_sync(0xffffffffu, asked, 0))) { ok = false; break; }
       }
-      if (GRAD && rank == 0 && ok && t.k_blocks == 0) {
-        taken = n_workers + __shfl_sync(0xffffffffu, asked, 0);
-        ok = announce(taken);
-        if (ok && lane == 0 && taken < total) asked = static_cast<int>(atomicAdd(p.counter, 1u));
-      }
+      if (GRAD && rank == 0 && ok && t.k_blocks == 0) ok = announce(n_workers + __shfl_sync(0xffffffffu, asked, 0));
     }
     if (!ok && rank == 0 && leader) {
       // giving up: what is still in flight gets the same limit to land
@@ -372,21 +403,12 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
-      int taken = worker;
-      for (bool begun = false; ok; begun = true) {
-        int i;
-        if (GRAD) {
-          i = next_announced();
-        } else {
-          if (begun) taken += n_workers;
-          i = taken < total ? taken : -1;
-        }
-        if (i < 0) break;
-        const Tile t = find_tile<GRAD>(p, work, i);
+      for (bool first = true; ok; first = false) {
+        if (GRAD ? !next_announced() : !next_static(first)) break;
         if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) break;
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kTile);
-        const bool mn_a = GRAD && t.kind == 2, mn_b = GRAD && t.kind != 0;
+        const bool mn_a = GRAD && t.kind == (p.by_words ? 1 : 2), mn_b = GRAD && t.kind != 0;
         const uint32_t idesc = umma_idesc_bf16(kTile, t.kind == 0 ? p.block_n : p.block_h) | (mn_a ? kAlongMnA : 0u) | (mn_b ? kAlongMnB : 0u);
         // 16 elements of K on: 32 bytes inside a row, or 16 rows
         const uint64_t step_a = mn_a ? 2048 >> 4 : 2, step_b = mn_b ? 2048 >> 4 : 2;
@@ -415,17 +437,8 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
     const uint32_t bar_acc_empty_0 = map_to_cta(bar_acc_empty, 0);
     int acc = 0;
     uint32_t acc_phase = 0;
-    int taken = worker;
-    for (bool begun = false;; begun = true) {
-      int i;
-      if (GRAD) {
-        i = next_announced();
-      } else {
-        if (begun) taken += n_workers;
-        i = taken < total ? taken : -1;
-      }
-      if (i < 0) break;
-      const Tile t = find_tile<GRAD>(p, work, i);
+    for (bool first = true;; first = false) {
+      if (GRAD ? !next_announced() : !next_static(first)) break;
       const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32;   // of this warp
       const int row = m0 + lane;
       const bool row_counts = row < rows;
@@ -445,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
         float top2 = kFloor, sum = 0.f;                 // largest logit times log2 e, sum of 2^(z log2 e - top2)
         const int n0 = t.n * p.block_n;
 #pragma unroll 1
-        for (int c = group * 32; c < p.block_n; c += 32 * kGroups) {
+        for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
           const int col = n0 + c;
           if (col >= p.vocab || m0 >= rows) break;
           uint32_t v[32];
@@ -477,13 +490,13 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
           for (int j = 0; j < 32; ++j) s[j & 3] += ex2_approx(fmaf(z[j], kLog2e, -top2));
           sum += (s[0] + s[1]) + (s[2] + s[3]);
         }
-        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + kGroups * t.n + group] = make_float2(top2, sum);
+        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + GROUPS * t.n + group] = make_float2(top2, sum);
       } else if (t.kind == 0) {
         const int n0 = t.n * p.block_n;                 // in the piece
         const bool whole = __all_sync(0xffffffffu, row_counts);
         bf16* g_out = p.g + static_cast<int64_t>(p.g_row0 + m0 + (lane & ~3)) * p.g_pitch + (lane & 3) * 8;
 #pragma unroll 1
-        for (int c = group * 32; c < p.block_n; c += 32 * kGroups) {
+        for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
           const int local = n0 + c;
           if (local >= p.cols || m0 >= work.row_k * 64) break;   // (kind 2 sums over rows in whole k-blocks)
           const int col = p.col0 + local;
@@ -497,12 +510,19 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
 #pragma unroll
           for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, minus_lse2));
           const int at = label - col;
-          if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+          const bool hit = __any_sync(0xffffffffu, at >= 0 && at < 32);
+          if (hit) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) if (j == at) g[j] -= 1.f;
           }
 #pragma unroll
           for (int j = 0; j < 32; ++j) g[j] *= weight;
+          if (hit) {                                    // what rounding takes from the label's entry
+            float mine = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) if (j == at) mine = g[j];
+            if (at >= 0 && at < 32) p.row_residual[row] = mine - __bfloat162float(__float2bfloat16_rn(mine));
+          }
           if (!whole) {                                 // (behind the last row lies anything)
 #pragma unroll
             for (int j = 0; j < 32; ++j) g[j] = row_counts ? g[j] : 0.f;
@@ -525,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
         const int n0 = t.n * p.block_h;
         float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * p.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
 #pragma unroll 1
-        for (int c = group * 32; c < p.block_h; c += 32 * kGroups) {
+        for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
           if (n0 + c >= p.hidden || m0 >= rows) break;
           uint32_t v[32];
           if (t.k_blocks > 0) {
@@ -556,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
         const int word = p.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
         bf16* dw = p.dw + static_cast<int64_t>(word) * p.dw_stride + (lane & 3) * 8;
 #pragma unroll 1
-        for (int c = group * 32; c < p.block_h; c += 32 * kGroups) {
+        for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
           const int col = n0 + c;
           if (col >= p.hidden || p.prev_col0 + m0 >= p.vocab) break;
           uint32_t v[32];
@@ -613,6 +633,269 @@ __global__ void __launch_bounds__(kThreads, 1) vocab_loss_pair_tcgen05(const __g
     __syncwarp();
     tc_fence_after();
     tmem_dealloc_pair(tmem_base, kTmemCols);
+  }
+}
+
+// ---- few rows ------------------------------------------------------------------------------------
+
+// Up to 128 rows the products are taken turned: 128 words are the rows (lanes) of an accumulator and the rows of x, rounded up to sixteen,
+// its columns, so that a tile costs what its rows cost and the kernel streams W: 16 KB of it per k-block and stage, up to twelve stages.
+// (20 rows x 30522 x 768 on tiles of 256 rows: 20 us, of which the tensor cores worked on empty rows for 6.)  An epilogue thread has one
+// word and all rows.
+//   forward   largest logit and sum of exponentials of a row over the 32 words of a warp: halves of the rows are exchanged for halves of the
+//             words (as column_sums), running over the CTA's tiles; the four warps are put together at the end
+//   backward  g by words, [vocab][64 or 128 rows], zeros in rows without a label and behind the last: as it is the operand along K for dW and
+//             the MN-major one for dx; db is a thread's own sum.  The hidden states are copied once with zeros in the rows without a label,
+//             for the product that sums over rows.
+constexpr int kFewRows = 128;
+constexpr int kFewThreads = 6 * 32;
+constexpr int kFewMaxStages = 12;
+constexpr int kFewStageA = 128 * 128;
+constexpr int kFewBook = 8192;
+constexpr int kFewRing = 227 * 1024 - 1024 - kFewBook;
+constexpr uint32_t kFewTmemCols = 256;
+
+// Largest over the 32 lanes of a warp of 32 columns each, column `lane` in the result (see column_sums).
+__device__ __forceinline__ float column_max(const float (&z)[32], int lane) {
+  float c[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const bool upper = (lane & 16) != 0;
+    const float give = upper ? z[i] : z[i + 16], keep = upper ? z[i + 16] : z[i];
+    c[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 16));
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    const bool upper = (lane & o) != 0;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float give = upper ? c[i] : c[i + o], keep = upper ? c[i + o] : c[i];
+      c[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, o));
+    }
+  }
+  return c[0];
+}
+
+template <bool GRAD>
+__global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid_constant__ VocabFewParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t ring = smem_u32(smem);
+  uint8_t* book = smem + kFewRing;
+  const uint32_t bar_full = smem_u32(book);
+  const uint32_t bar_empty = bar_full + 8 * kFewMaxStages;
+  const uint32_t bar_acc_full = bar_empty + 8 * kFewMaxStages;
+  const uint32_t bar_acc_empty = bar_acc_full + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * kFewMaxStages + 4));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* s_label = reinterpret_cast<int*>(book + 256);                    // of every row; -1 where it takes no part
+  float2* s_row = reinterpret_cast<float2*>(book + 256 + 512);          // (backward) -lse log2 e, weight
+  float2* s_part = reinterpret_cast<float2*>(book + 256 + 512 + 1024);  // (forward) [quarter][row]
+  static_assert(256 + 512 + 1024 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int stages = p.stages, stage_bytes = p.stage_bytes;
+  const int k_blocks = (p.hidden + 63) / 64;
+  const int tiles = (p.vocab + 127) / 128;
+  if (tid == 0) {
+    for (int s = 0; s < kFewMaxStages; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(bar_acc_full + 8 * a, 1);
+      mbar_init(bar_acc_empty + 8 * a, 4);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_shared();
+    prefetch_tensormap(&p.x_k);
+    prefetch_tensormap(&p.w_k);
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), kFewTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dependency_wait();
+  grid_launch_dependents();
+
+  if (warp == 0) {
+    // ------------------------------ TMA producer ------------------------------
+    const bool leader = elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    long long issued = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+      for (int kb = 0; kb < k_blocks; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag))) { ok = false; break; }
+        if (leader) {
+          const uint32_t a = ring + stage * stage_bytes;
+          mbar_expect_tx(bar_full + 8 * stage, stage_bytes);
+          tma_load_2d(a, &p.w_k, kb * 64, tile * 128, bar_full + 8 * stage);
+          tma_load_2d(a + kFewStageA, &p.x_k, kb * 64, 0, bar_full + 8 * stage);
+        }
+        ++issued;
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok && leader) {
+      const int pending = issued < stages ? static_cast<int>(issued) : stages;
+      for (int i = 0; i < pending; ++i) {
+        if (stage == 0) { stage = stages; phase ^= 1u; }
+        --stage;
+        mbar_drain(bar_full + 8 * stage, phase);
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------ MMA issuer --------------------------------
+    const bool leader = elect_one();
+    const uint32_t idesc = umma_idesc_bf16(128, p.columns);
+    int stage = 0, acc = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) break;
+      tc_fence_after();
+      const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kFewRows);
+      for (int kb = 0; kb < k_blocks; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
+        tc_fence_after();
+        if (leader) {
+          const uint64_t da = smem_desc_sw128(ring + stage * stage_bytes), db = smem_desc_sw128(ring + stage * stage_bytes + kFewStageA);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) umma_bf16(d_tmem, da + 2 * k, db + 2 * k, idesc, (kb | k) != 0 ? 1u : 0u);
+          umma_commit(bar_empty + 8 * stage);
+        }
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
+      if (!ok) break;
+      if (leader) umma_commit(bar_acc_full + 8 * acc);
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    }
+  } else {
+    // ------------------------------ epilogue ----------------------------------
+    const int quarter = warp & 3;
+    const int row0 = tid - 64;                                      // the row that this thread fetches the label of
+    int label = row0 < p.rows ? p.labels[row0] : -1;
+    if (GRAD && label >= p.vocab && blockIdx.x == 0 && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
+    if (label >= p.vocab) label = -1;
+    s_label[row0] = label;
+    if (GRAD)
+      s_row[row0] = label >= 0 ? make_float2(-p.lse[row0] * kLog2e, p.grad_loss != nullptr ? p.grad_loss[row0] : 1.f) : make_float2(0.f, 0.f);
+    asm volatile("bar.sync 1, 128;" ::: "memory");                 // (the epilogue warps; nothing that can give up comes before it)
+    if (GRAD && p.x_clean != nullptr) {
+      // (rows of hidden states, those without a part as zeros, in whole k-blocks of the product over rows)
+      const int vectors = p.hidden / 8;
+      for (int r = blockIdx.x; r < p.g_pitch; r += gridDim.x) {
+        const bool there = s_label[r] >= 0;
+        for (int c = row0; c < vectors; c += 128)
+          reinterpret_cast<uint4*>(p.x_clean + static_cast<int64_t>(r) * p.hidden)[c] =
+              there ? __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(r) * p.x_stride) + c) : make_uint4(0, 0, 0, 0);
+      }
+    }
+    if (GRAD && blockIdx.x == 0 && row0 == 0) *p.counter = 0;
+    float2* my_part = s_part + quarter * kFewRows + lane;           // (forward) largest logit and sum of row 32 * i + lane
+    if (!GRAD) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) my_part[i * 32] = make_float2(kFloor, 0.f);
+    }
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+      const int word0 = tile * 128 + quarter * 32, word = word0 + lane;
+      const bool is_word = word < p.vocab;
+      const float bias = p.bias != nullptr && is_word ? __bfloat162float(p.bias[word]) : 0.f;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * acc, acc_phase, abort_flag))) break;
+      tc_fence_after();
+      const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc * kFewRows);
+      float db = 0.f;
+      const int chunks = ((GRAD ? p.g_pitch : p.rows) + 31) / 32;
+      // (not unrolled: four copies of the body are more than the instruction cache holds; the first tile took 13 k clocks with them)
+#pragma unroll 1
+      for (int i = 0; i < chunks; ++i) {
+        uint32_t v[32];
+        tmem_ld_32x32(taddr0 + i * 32, v);
+        tmem_ld_wait();
+        float z[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]) + bias;
+        const int my_label = s_label[i * 32 + lane];                // of row i * 32 + lane
+        // rows whose label is one of this warp's words
+        uint32_t hits = __ballot_sync(0xffffffffu, my_label >= word0 && my_label < word0 + 32);
+        if (!GRAD) {
+          if (hits != 0) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              if ((hits >> j) & 1u) {
+                if (s_label[i * 32 + j] == word) p.label_logit[i * 32 + j] = z[j];
+              }
+            }
+          }
+          if (!is_word) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z[j] = -INFINITY;
+          }
+          const float2 part = my_part[i * 32];
+          const float next2 = fmaxf(part.x, column_max(z, lane) * kLog2e);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = ex2_approx(fmaf(z[j], kLog2e, -__shfl_sync(0xffffffffu, next2, j)));
+          my_part[i * 32] = make_float2(next2, part.y * ex2_approx(part.x - next2) + column_sums(z, lane));
+        } else {
+          const uint32_t counts = __ballot_sync(0xffffffffu, my_label >= 0);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = ex2_approx(fmaf(z[j], kLog2e, s_row[i * 32 + j].x));
+          if (hits != 0) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              if (((hits >> j) & 1u) && s_label[i * 32 + j] == word) {
+                z[j] -= 1.f;
+                const float entry = z[j] * s_row[i * 32 + j].y;      // what rounding takes from the label's entry
+                p.row_residual[i * 32 + j] = entry - __bfloat162float(__float2bfloat16_rn(entry));
+              }
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = ((counts >> j) & 1u) && is_word ? z[j] * s_row[i * 32 + j].y : 0.f;
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[j & 3] += z[j];
+          db += (s[0] + s[1]) + (s[2] + s[3]);
+          uint4 out[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            out[q] = make_uint4(pack_bf16(z[q * 8], z[q * 8 + 1]), pack_bf16(z[q * 8 + 2], z[q * 8 + 3]), pack_bf16(z[q * 8 + 4], z[q * 8 + 5]),
+                                pack_bf16(z[q * 8 + 6], z[q * 8 + 7]));
+          exchange_pieces(out, lane);
+          bf16* g = p.g + static_cast<int64_t>(word0 + (lane & ~3)) * p.g_pitch + i * 32 + (lane & 3) * 8;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g + q * p.g_pitch) = out[q];
+        }
+      }
+      if (GRAD && p.db != nullptr && is_word) p.db[word] = p.accumulate ? p.db[word] + db : db;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_acc_empty + 8 * acc);
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (!GRAD && tid < p.rows) {
+    float top = kFloor, sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) top = fmaxf(top, s_part[q * kFewRows + tid].x);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum += s_part[q * kFewRows + tid].y * ex2_approx(s_part[q * kFewRows + tid].x - top);
+    p.parts[tid * p.part_pitch + blockIdx.x] = make_float2(top, sum);
+  }
+  if (tid == 0 && *abort_flag && p.status != nullptr) atomicOr(p.status, kFlagWaitTimeout);
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kFewTmemCols);
   }
 }
 
@@ -747,8 +1030,9 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __g
   }
 }
 
-// dx: the ranges of a row added up in order, rounded once, to the row's place; zeros for rows without a label.  A warp per row and 256
-// columns.
+// dx: the ranges of a row added up in order, and what rounding took from the label's entry of g times the label's row of W (that one entry
+// is most of a row of g: without this a row of dx would be off by its rounding); rounded once, to the row's place; zeros for rows without
+// a label.  A warp per row and 256 columns.
 __global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_constant__ VocabDxParams p) {
   grid_dependency_wait();
   grid_launch_dependents();
@@ -758,10 +1042,14 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_con
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); u < units; u += step) {
     const int row = static_cast<int>(u / blocks), c = static_cast<int>(u % blocks) * 256 + lane * 8;
     if (c >= p.hidden) continue;
-    const int place = p.place_of[row];
+    const int label = p.labels[row];
+    const bool counts = label >= 0 && label < p.vocab;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-    if (place >= 0) {
+    if (counts) {
+      const int place = p.place_of != nullptr ? p.place_of[row] : row;
       const float* src = p.sums + static_cast<int64_t>(place) * p.hidden + c;
+      const uint4 word = __ldg(reinterpret_cast<const uint4*>(p.w + static_cast<int64_t>(label) * p.w_stride + c));
+      const float residual = p.row_residual[place];
 #pragma unroll 8
       for (int s = 0; s < p.ranges; ++s) {
         const float4* f = reinterpret_cast<const float4*>(src + static_cast<int64_t>(s) * p.row_pitch * p.hidden);
@@ -769,6 +1057,10 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_con
         a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
         b.x += w.x; b.y += w.y; b.z += w.z; b.w += w.w;
       }
+      a.x = fmaf(residual, bf16_lo(word.x), a.x); a.y = fmaf(residual, bf16_hi(word.x), a.y);
+      a.z = fmaf(residual, bf16_lo(word.y), a.z); a.w = fmaf(residual, bf16_hi(word.y), a.w);
+      b.x = fmaf(residual, bf16_lo(word.z), b.x); b.y = fmaf(residual, bf16_hi(word.z), b.y);
+      b.z = fmaf(residual, bf16_lo(word.w), b.z); b.w = fmaf(residual, bf16_hi(word.w), b.w);
     }
     *reinterpret_cast<uint4*>(p.dx + static_cast<int64_t>(row) * p.dx_stride + c) =
         make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
@@ -797,6 +1089,23 @@ __global__ void __launch_bounds__(256) vocab_bias_kernel(const __grid_constant__
 }
 
 template <bool GRAD>
+cudaError_t launch_few(VocabFewParams p, int sm_count, int* ctas, cudaStream_t stream) {
+  auto kernel = vocab_few_tcgen05<GRAD>;
+  static PerDeviceOnce once;
+  cudaError_t err = per_device_once(once, [&](int) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewRing + kFewBook + 1024);
+  });
+  if (err != cudaSuccess) return err;
+  p.columns = (p.rows + 15) / 16 * 16;
+  p.stage_bytes = kFewStageA + p.columns * 128;
+  p.stages = kFewRing / p.stage_bytes < kFewMaxStages ? kFewRing / p.stage_bytes : kFewMaxStages;
+  const int tiles = (p.vocab + 127) / 128;
+  *ctas = tiles < sm_count ? tiles : (sm_count > 0 ? sm_count : 1);
+  if (!GRAD) p.part_pitch = *ctas;
+  return launch_kernel(kernel, dim3(*ctas), dim3(kFewThreads), kFewRing + kFewBook + 1024, stream, p);
+}
+
+template <bool GRAD>
 cudaError_t launch_pairs(const VocabLossParams& p, int tiles, int sm_count, cudaStream_t stream) {
   auto kernel = vocab_loss_pair_tcgen05<GRAD>;
   static PerDeviceOnce once;
@@ -806,7 +1115,7 @@ cudaError_t launch_pairs(const VocabLossParams& p, int tiles, int sm_count, cuda
   if (err != cudaSuccess) return err;
   const int most = sm_count / 2 > 0 ? sm_count / 2 : 1;
   const int workers = tiles < most ? (tiles > 0 ? tiles : 1) : most;
-  return launch_kernel(kernel, dim3(2 * workers), dim3(kThreads), kSmemBytes, stream, p, 2u);
+  return launch_kernel(kernel, dim3(2 * workers), dim3(threads(GRAD)), kSmemBytes, stream, p, 2u);
 }
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
@@ -815,6 +1124,7 @@ size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
 // ---- plans -----------------------------------------------------------------------------------------
 
 constexpr int kGatherRows = kTile;       // up to one tile of rows costs the same however few of them count
+constexpr int kFewPartCtas = 256;        // place for the CTAs of the kernel for few rows
 constexpr int64_t kPieceElements = 32 << 20;   // of g of one piece: 64 MB
 constexpr int kMinPiece = 2048;
 constexpr int kMaxRanges = 32;
@@ -841,31 +1151,36 @@ ForwardPlan forward_plan(int rows, int vocab, int hidden, int sm_count) {
     if (best < 0 || cost < best) { best = cost; f.block_n = bn; }
   }
   f.tiles_n = ceil_div(vocab, f.block_n);
-  f.part_pitch = kGroups * f.tiles_n;
+  f.part_pitch = groups(false) * f.tiles_n;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += whole_lines(bytes); return here; };
   f.count = take(256);
   f.row_of = take(f.row_pitch * 4);
   f.row_label = take(f.row_pitch * 4);
   f.label_logit = take(f.row_pitch * 4);
-  f.parts = take(static_cast<size_t>(f.row_pitch) * ceil_div(vocab, kHalf) * kGroups * sizeof(float2));   // (for the narrowest tiles)
+  const size_t parts_of_row = rows <= kFewRows ? kFewPartCtas : static_cast<size_t>(ceil_div(vocab, kHalf)) * groups(false);   // (for the narrowest tiles)
+  f.parts = take(static_cast<size_t>(f.row_pitch) * parts_of_row * sizeof(float2));
   f.gathered = take(f.gather ? static_cast<size_t>(f.row_pitch) * hidden * 2 : 0);
   f.bytes = at;
   return f;
 }
 
 struct GradPlan {
-  int piece, pieces, buffers, block_h, ranges;
+  int piece, pieces, buffers, block_h, ranges, g_pitch;
+  bool few;
   int64_t row_pitch;
-  size_t count, counters, row_of, row_label, row_lse, row_weight, place_of, gathered, g, dx, bias_parts, bytes;
+  size_t count, counters, row_of, row_label, row_lse, row_weight, row_residual, place_of, gathered, g, dx, bias_parts, bytes;
 };
 GradPlan grad_plan(int rows, int vocab, int hidden) {
   GradPlan f;
   f.row_pitch = static_cast<int64_t>(ceil_div(rows, kTile)) * kTile;
   const int m = static_cast<int>(f.row_pitch / kTile);
   const int64_t all = static_cast<int64_t>(ceil_div(vocab, kTile)) * kTile;
+  f.few = rows <= kFewRows;
+  f.g_pitch = (rows + 63) / 64 * 64;       // (few rows: g is kept by words)
   int64_t piece = kPieceElements / (f.row_pitch > 0 ? f.row_pitch : 1) / kTile * kTile;
   if (piece < kMinPiece) piece = kMinPiece;
+  if (f.few) piece = all;
   f.pieces = ceil_div(all, piece);
   f.piece = static_cast<int>(ceil_div(all / kTile, f.pieces)) * kTile;      // (pieces of the same size)
   f.pieces = ceil_div(all, f.piece);
@@ -889,11 +1204,12 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.row_label = take(f.row_pitch * 4);
   f.row_lse = take(f.row_pitch * 4);
   f.row_weight = take(f.row_pitch * 4);
+  f.row_residual = take(f.row_pitch * 4);
   f.place_of = take(f.row_pitch * 4);
   f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
-  f.g = take(static_cast<size_t>(f.buffers) * f.row_pitch * f.piece * 2);
+  f.g = take(static_cast<size_t>(f.buffers) * (f.few ? f.g_pitch : f.row_pitch) * f.piece * 2);
   f.dx = take(static_cast<size_t>(f.ranges) * f.row_pitch * hidden * 4);
-  f.bias_parts = take(static_cast<size_t>(f.row_pitch / 32) * vocab * 4);
+  f.bias_parts = take(f.few ? 0 : static_cast<size_t>(f.row_pitch / 32) * vocab * 4);
   f.bytes = at;
   return f;
 }
@@ -915,6 +1231,21 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
   const ForwardPlan f = forward_plan(c.rows, c.vocab, c.hidden, sm_count);
   void* ws = c.workspace;
   cudaError_t e;
+  if (c.rows <= kFewRows) {
+    VocabFewParams w;
+    memset(&w, 0, sizeof(w));
+    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
+    w.label_logit = at<float>(ws, f.label_logit); w.parts = at<float2>(ws, f.parts);
+    if ((e = encode_matrix_map(&w.x_k, c.x, c.rows, c.hidden, c.x_stride * 2, ceil_div(c.rows, 16) * 16, 64, false)) != cudaSuccess ||
+        (e = encode_matrix_map(&w.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, 128, 64, false)) != cudaSuccess)
+      return e;
+    VocabJoinParams j;
+    memset(&j, 0, sizeof(j));
+    if ((e = launch_few<false>(w, sm_count < kFewPartCtas ? sm_count : kFewPartCtas, &j.n_parts, stream)) != cudaSuccess) return e;
+    j.part_pitch = j.n_parts; j.labels = c.labels; j.parts = w.parts; j.label_logit = w.label_logit; j.loss = c.loss; j.lse = c.lse_out;
+    j.rows = c.rows; j.vocab = c.vocab; j.status = c.status;
+    return launch_kernel(vocab_loss_join_kernel, dim3(ceil_div(c.rows, kJoinThreads / 32)), dim3(kJoinThreads), 0, stream, j);
+  }
   if (f.gather) {
     VocabRowsParams r;
     memset(&r, 0, sizeof(r));
@@ -951,6 +1282,50 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   const GradPlan f = grad_plan(c.rows, c.vocab, c.hidden);
   void* ws = c.workspace;
   cudaError_t e;
+  VocabDxParams d;
+  memset(&d, 0, sizeof(d));
+  d.sums = at<float>(ws, f.dx); d.labels = c.labels; d.row_residual = at<float>(ws, f.row_residual); d.w = c.w; d.w_stride = c.w_stride;
+  d.dx = c.dx; d.dx_stride = c.dx_stride; d.rows = c.rows; d.vocab = c.vocab; d.hidden = c.hidden; d.row_pitch = f.row_pitch; d.ranges = f.ranges;
+  const int64_t dx_units = (static_cast<int64_t>(c.rows) * ceil_div(c.hidden, 256) + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
+  const dim3 dx_ctas(static_cast<unsigned>(dx_units < 16 * sm_count ? dx_units : 16 * sm_count));
+  bf16* gathered = at<bf16>(ws, f.gathered);
+  bf16* g = at<bf16>(ws, f.g);
+  const int64_t h_stride = static_cast<int64_t>(c.hidden) * 2;
+  const bool products = c.dx != nullptr || c.dw != nullptr;
+  const int row_tiles = static_cast<int>(f.row_pitch / kTile), hidden_tiles = ceil_div(c.hidden, f.block_h);
+  VocabLossParams p;
+  memset(&p, 0, sizeof(p));
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias; p.status = c.status;
+  p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.dx_sums = at<float>(ws, f.dx);
+  p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate;
+  p.dw = c.dw; p.dw_stride = c.dw_stride;
+  if ((e = encode_matrix_map(&p.w_mn, c.w, c.vocab, c.hidden, c.w_stride * 2, 64, 64, false)) != cudaSuccess) return e;
+
+  if (f.few) {
+    VocabFewParams w;
+    memset(&w, 0, sizeof(w));
+    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
+    w.lse = c.lse; w.grad_loss = c.grad_loss; w.x = c.x; w.x_stride = c.x_stride; w.x_clean = c.dw != nullptr ? gathered : nullptr;
+    w.g = g; w.g_pitch = f.g_pitch; w.db = c.db; w.accumulate = c.accumulate; w.row_residual = at<float>(ws, f.row_residual);
+    w.counter = at<uint32_t>(ws, f.counters);
+    if ((e = encode_matrix_map(&w.x_k, c.x, c.rows, c.hidden, c.x_stride * 2, ceil_div(c.rows, 16) * 16, 64, false)) != cudaSuccess ||
+        (e = encode_matrix_map(&w.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, 128, 64, false)) != cudaSuccess)
+      return e;
+    int ctas = 0;
+    if ((e = launch_few<true>(w, sm_count, &ctas, stream)) != cudaSuccess || !products) return e;
+    const int words = ceil_div(c.vocab, 128) * 128;
+    if ((e = encode_matrix_map(&p.g_k, g, words, f.g_pitch, f.g_pitch * 2, kHalf, 64, false)) != cudaSuccess ||
+        (e = encode_matrix_map(&p.g_mn, g, words, f.g_pitch, f.g_pitch * 2, 64, 64, false)) != cudaSuccess ||
+        (e = encode_matrix_map(&p.x_mn[0], gathered, f.g_pitch, c.hidden, h_stride, 64, 64, false)) != cudaSuccess)
+      return e;
+    p.x_mn[1] = p.x_mn[0];
+    p.x_k[0] = p.w_k = p.w_mn;      // (of kind 0, which has no tiles here)
+    p.by_words = 1; p.prev_cols = c.vocab; p.prev_first = 1; p.counter = w.counter;
+    const int tiles = row_tiles * hidden_tiles * f.ranges + ceil_div(c.vocab, kTile) * hidden_tiles;
+    if ((e = launch_pairs<true>(p, tiles, sm_count, stream)) != cudaSuccess || c.dx == nullptr) return e;
+    return launch_kernel(vocab_dx_kernel, dx_ctas, dim3(kJoinThreads), 0, stream, d);
+  }
+
   VocabRowsParams r;
   memset(&r, 0, sizeof(r));
   r.labels = c.labels; r.x = c.x; r.x_stride = c.x_stride; r.rows = c.rows; r.vocab = c.vocab; r.hidden = c.hidden;
@@ -962,27 +1337,16 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   launch_rows_setup(&r, &ctas);
   if ((e = launch_kernel(vocab_rows_kernel, dim3(ctas), dim3(kRowsThreads), 0, stream, r)) != cudaSuccess) return e;
 
-  VocabLossParams p;
-  memset(&p, 0, sizeof(p));
-  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias;
-  p.labels = r.row_label; p.count = r.count; p.row_lse = r.row_lse; p.row_weight = r.row_weight;
-  p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.status = c.status;
-  p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate;
-  p.dw = c.dw; p.dw_stride = c.dw_stride;
+  p.labels = r.row_label; p.count = r.count; p.row_lse = r.row_lse; p.row_weight = r.row_weight; p.row_residual = at<float>(ws, f.row_residual);
   p.bias_parts = c.db != nullptr ? at<float>(ws, f.bias_parts) : nullptr; p.bias_pitch = c.vocab;
-  bf16* gathered = at<bf16>(ws, f.gathered);
-  bf16* g = at<bf16>(ws, f.g);
-  const int64_t g_rows = f.buffers * f.row_pitch, g_stride = static_cast<int64_t>(f.piece) * 2, h_stride = static_cast<int64_t>(c.hidden) * 2;
+  p.g = g; p.g_pitch = f.piece;
+  const int64_t g_rows = f.buffers * f.row_pitch, g_stride = static_cast<int64_t>(f.piece) * 2;
   if ((e = encode_matrix_map(&p.x_k[0], c.x, c.rows, c.hidden, c.x_stride * 2, kHalf, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_k[1], gathered, f.row_pitch, c.hidden, h_stride, kHalf, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_mn[0], c.x, c.rows, c.hidden, c.x_stride * 2, 64, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_mn[1], gathered, f.row_pitch, c.hidden, h_stride, 64, 64, false)) != cudaSuccess ||
-      (e = encode_matrix_map(&p.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, kHalf, 64, false)) != cudaSuccess ||
-      (e = encode_matrix_map(&p.w_mn, c.w, c.vocab, c.hidden, c.w_stride * 2, 64, 64, false)) != cudaSuccess)
+      (e = encode_matrix_map(&p.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, kHalf, 64, false)) != cudaSuccess)
     return e;
-  p.g = g; p.g_pitch = f.piece; p.dx_sums = at<float>(ws, f.dx);
-  const bool products = c.dx != nullptr || c.dw != nullptr;
-  const int row_tiles = static_cast<int>(f.row_pitch / kTile), hidden_tiles = ceil_div(c.hidden, f.block_h);
   for (int j = 0; j <= f.pieces; ++j) {
     if (j == f.pieces && !products) break;
     p.col0 = j * f.piece;
@@ -1008,12 +1372,8 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     if ((e = launch_kernel(vocab_bias_kernel, dim3(ceil_div(c.vocab, 32)), dim3(256), 0, stream, b)) != cudaSuccess) return e;
   }
   if (c.dx == nullptr) return cudaSuccess;
-  VocabDxParams d;
-  memset(&d, 0, sizeof(d));
-  d.sums = at<float>(ws, f.dx); d.place_of = r.place_of; d.dx = c.dx; d.dx_stride = c.dx_stride; d.rows = c.rows; d.hidden = c.hidden;
-  d.row_pitch = f.row_pitch; d.ranges = f.ranges;
-  const int64_t dx_ctas = (static_cast<int64_t>(c.rows) * ceil_div(c.hidden, 256) + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
-  return launch_kernel(vocab_dx_kernel, dim3(static_cast<unsigned>(dx_ctas < 16 * sm_count ? dx_ctas : 16 * sm_count)), dim3(kJoinThreads), 0, stream, d);
+  d.place_of = r.place_of;
+  return launch_kernel(vocab_dx_kernel, dx_ctas, dim3(kJoinThreads), 0, stream, d);
 }
 
 }  // namespace mt
