@@ -472,13 +472,23 @@ size_t vocab_loss_grad_workspace(int rows, int vocab, int hidden);
 cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t stream);
 cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStream_t stream);
 
+// How a gradient is cut up, decided on the device from the number of rows with a label.
+struct VocabPlan {
+  int32_t rows;                // with a label
+  int32_t shift;               // pieces are this many powers of two wider than for all rows
+  int32_t piece, pieces;       // columns of a piece of the vocabulary, and how many there are
+  int32_t ranges;              // of a piece, that dx is summed over in
+  int32_t row_pitch;           // rows in whole tiles
+};
+constexpr int kVocabShifts = 4;
 // The products.  Index 1 of the maps of x: the rows with a label, gathered.  Boxes of 128 x 64 (block_n / 2 x 64) for operands along K,
 // 64 x 64 for operands whose rows run along K.
 struct VocabLossParams {
-  CUtensorMap x_k[2], w_k, x_mn[2], w_mn, g_k, g_mn;
+  CUtensorMap x_k[2], w_k, x_mn[2], w_mn, g_k[kVocabShifts], g_mn[kVocabShifts];   // (g: by VocabPlan::shift)
   const bf16* bias;
   const int32_t* labels;       // of the rows in use
-  const int32_t* count;        // rows in use (or null: rows)
+  const int32_t* count;        // forward: rows in use (or null: rows)
+  const VocabPlan* plan;       // backward (null: few rows, and what follows is given)
   const float* row_lse;
   const float* row_weight;
   float* row_residual;         // backward: what rounding takes from the label's entry of g
@@ -492,13 +502,10 @@ struct VocabLossParams {
   uint32_t* counter;           // next tile to hand out
   uint32_t* status;
   int32_t rows, vocab, hidden, block_n, block_h;
-  int32_t col0, cols;          // columns of the vocabulary whose logits are taken
-  int32_t prev_col0, prev_cols;   // columns whose g is taken into the products (0: none)
-  int32_t g_row0, prev_g_row0; // first row of their buffers of g
-  int32_t row_pitch;           // rows in whole tiles
-  int32_t ranges;              // of the vocabulary, for dx
-  int32_t prev_first;          // dx is stored, not added to
-  int32_t part_pitch, bias_pitch, g_pitch;
+  int32_t index;               // backward: of the launch: g of this piece, the products of the one before
+  int32_t buffers, buffer_rows;   // of g, at shift 0
+  int32_t row_pitch, ranges;   // (few rows)
+  int32_t part_pitch, bias_pitch;
   int32_t want_x, want_w, accumulate;
   int32_t by_words;            // g lies by words, [vocab][rows] (few rows; g_k: boxes of 128 words, g_mn: of 64)
 };
@@ -529,6 +536,8 @@ struct VocabRowsParams {
   const float* grad_loss;
   int64_t x_stride;
   int32_t rows, vocab, hidden, rows_per_cta, n_counters;
+  VocabPlan* plan;             // backward; or null.  From what there is place for:
+  int32_t piece, max_shift, buffer_rows, dx_rows, block_h;
   int32_t* count;
   uint32_t* counters;          // set to zero
   int32_t* row_of;             // caller's row of a row in use
@@ -553,6 +562,7 @@ struct VocabJoinParams {
   uint32_t* status;
 };
 struct VocabDxParams {
+  const VocabPlan* plan;       // (null: ranges and row_pitch as given)
   const float* sums;           // [ranges][row_pitch][hidden]
   const int32_t* place_of;     // or null: in place
   const int32_t* labels;

@@ -44,6 +44,7 @@ constexpr int kSlots = 4;                  // tiles announced ahead
 constexpr uint32_t kTmemCols = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kMaxRanges = 32;             // of the vocabulary, for dx
 constexpr float kFloor = -1e30f;           // below every logit that counts; finite, so that -inf minus it is no NaN
 
 // All of shared memory is the ring: what a pair computes is bound by how many bytes are on their way (32 KB per k-block and CTA, of the 64
@@ -100,12 +101,53 @@ __device__ __forceinline__ void send_words(uint32_t cluster_addr, int a, int b, 
                : "memory");
 }
 
+// What a launch works on.
+struct Span {
+  int rows;                    // in use
+  int col0, cols;              // columns of the vocabulary whose logits are taken
+  int prev_col0, prev_cols;    // (backward) columns whose g is taken into the products
+  int g_row0, prev_g_row0;     // first row of their buffers of g
+  int g_pitch, shift;
+  int ranges, row_pitch;
+};
+template <bool GRAD>
+__device__ __forceinline__ Span make_span(const VocabLossParams& p) {
+  Span s = {};
+  if (!GRAD) {
+    s.rows = p.count != nullptr ? min(p.rows, *reinterpret_cast<const volatile int*>(p.count)) : p.rows;
+    s.cols = p.vocab;
+  } else if (p.plan == nullptr) {
+    s.rows = p.rows;
+    s.prev_cols = p.vocab;
+    s.ranges = p.ranges;
+    s.row_pitch = p.row_pitch;
+  } else {
+    const volatile VocabPlan* plan = p.plan;
+    s.rows = plan->rows;
+    s.shift = plan->shift;
+    s.ranges = plan->ranges;
+    s.row_pitch = plan->row_pitch;
+    s.g_pitch = plan->piece;
+    const int pieces = plan->pieces;
+    if (p.index < pieces) {
+      s.col0 = p.index * s.g_pitch;
+      s.cols = min(s.g_pitch, p.vocab - s.col0);
+      s.g_row0 = (p.index & (p.buffers - 1)) * (p.buffer_rows >> s.shift);
+    }
+    if (p.index > 0 && p.index <= pieces) {
+      s.prev_col0 = (p.index - 1) * s.g_pitch;
+      s.prev_cols = min(s.g_pitch, p.vocab - s.prev_col0);
+      s.prev_g_row0 = ((p.index - 1) & (p.buffers - 1)) * (p.buffer_rows >> s.shift);
+    }
+  }
+  return s;
+}
+
 // The tiles of a launch, in the order in which they are handed out: long ones first.
 struct Work {
   int row_tiles;               // 256 rows each
   int n0, n1, n2;              // tiles of each kind
   int k0, k1, k2;              // their k-blocks (k1: of one range of the vocabulary)
-  int row_k;                   // k-blocks that cover the rows
   bool first1;                 // kind 1 before kind 2
   int hidden_tiles;
 };
@@ -114,29 +156,28 @@ struct Tile {
 };
 
 template <bool GRAD>
-__device__ __forceinline__ Work make_work(const VocabLossParams& p, int rows) {
+__device__ __forceinline__ Work make_work(const VocabLossParams& p, const Span& s) {
   Work w;
-  w.row_tiles = (rows + kTile - 1) / kTile;
-  w.n0 = w.row_tiles * ((p.cols + p.block_n - 1) / p.block_n);
+  w.row_tiles = (s.rows + kTile - 1) / kTile;
+  w.n0 = w.row_tiles * ((s.cols + p.block_n - 1) / p.block_n);
   w.k0 = (p.hidden + 63) / 64;
   w.n1 = w.n2 = w.k1 = w.k2 = 0;
-  w.row_k = (rows + 63) / 64;
   w.first1 = false;
   w.hidden_tiles = 1;
   if (GRAD) {
     w.hidden_tiles = (p.hidden + p.block_h - 1) / p.block_h;
-    if (p.prev_cols > 0) {
-      if (p.want_x) w.n1 = w.row_tiles * w.hidden_tiles * p.ranges;
-      if (p.want_w) w.n2 = (p.prev_cols + kTile - 1) / kTile * w.hidden_tiles;
-      w.k1 = ((p.prev_cols + 63) / 64 + p.ranges - 1) / p.ranges;
-      w.k2 = w.row_k;
+    if (s.prev_cols > 0) {
+      if (p.want_x) w.n1 = w.row_tiles * w.hidden_tiles * s.ranges;
+      if (p.want_w) w.n2 = (s.prev_cols + kTile - 1) / kTile * w.hidden_tiles;
+      w.k1 = ((s.prev_cols + 63) / 64 + s.ranges - 1) / s.ranges;
+      w.k2 = (s.rows + 63) / 64;
       w.first1 = w.k1 > w.k2;
     }
   }
   return w;
 }
 template <bool GRAD>
-__device__ __forceinline__ Tile find_tile(const VocabLossParams& p, const Work& w, int i) {
+__device__ __forceinline__ Tile find_tile(const Span& s, const Work& w, int i) {
   Tile t;
   t.range = 0;
   t.k_begin = 0;
@@ -150,7 +191,7 @@ __device__ __forceinline__ Tile find_tile(const VocabLossParams& p, const Work& 
       t.n = i % w.hidden_tiles;
       t.range = i / w.hidden_tiles;
       t.k_begin = t.range * w.k1;
-      const int all = (p.prev_cols + 63) / 64;
+      const int all = (s.prev_cols + 63) / 64;
       t.k_blocks = all - t.k_begin < w.k1 ? (all > t.k_begin ? all - t.k_begin : 0) : w.k1;
     } else {
       if (w.first1) i -= w.n1;
@@ -258,25 +299,24 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
   const uint32_t bar_full_count = map_to_cta(bar_full, 0);
   const uint32_t bar_slot_empty_0 = map_to_cta(bar_slot_empty, 0);
   if (warp == 0 && lane == 0) {
-    if (!GRAD || p.cols > 0) {
-      prefetch_tensormap(&p.x_k[0]);
-      prefetch_tensormap(&p.w_k);
-    }
-    if (GRAD && p.prev_cols > 0) {
+    prefetch_tensormap(&p.x_k[0]);
+    prefetch_tensormap(&p.w_k);
+    if (GRAD) {
       prefetch_tensormap(&p.w_mn);
-      prefetch_tensormap(&p.g_k);
-      prefetch_tensormap(&p.g_mn);
+      prefetch_tensormap(&p.g_k[0]);
+      prefetch_tensormap(&p.g_mn[0]);
       prefetch_tensormap(&p.x_mn[0]);
     }
   }
   // (a first look at each line of the arguments costs some hundred clocks: before the wait, not after)
-  asm volatile("" ::"r"(p.rows), "r"(p.cols), "r"(p.block_n), "r"(p.block_h), "r"(p.prev_cols), "r"(p.row_pitch), "r"(p.ranges), "r"(p.want_w),
+  asm volatile("" ::"r"(p.rows), "r"(p.block_n), "r"(p.block_h), "r"(p.index), "r"(p.want_w),
                "l"(p.labels), "l"(p.counter));
   grid_dependency_wait();
   grid_launch_dependents();
-  const int rows = p.count != nullptr ? min(p.rows, *reinterpret_cast<const volatile int*>(p.count)) : p.rows;
+  const Span span = make_span<GRAD>(p);
+  const int rows = span.rows;
   const int gathered = rows == p.rows ? 0 : 1;      // which x: the caller's, or the rows with a label
-  const Work work = make_work<GRAD>(p, rows);
+  const Work work = make_work<GRAD>(p, span);
   const int total = work.n0 + work.n1 + work.n2;
 
   // Tiles.  Forward: worker, worker + n_workers, ... (all tiles cost the same).  Backward: the next of the list, whoever is free first;
@@ -328,7 +368,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
     int asked = 0;
     Tile ahead = t;
     auto announce = [&](int i) -> bool {
-      if (i < total) ahead = find_tile<GRAD>(p, work, i); else ahead.kind = -1;
+      if (i < total) ahead = find_tile<GRAD>(span, work, i); else ahead.kind = -1;
       if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) return false;
       if (lane < 2)
         send_words(map_to_cta(smem_u32(const_cast<int4*>(slot_tile) + slot), lane), ahead.kind, ahead.m, ahead.n | (ahead.range << 16), ahead.k_blocks,
@@ -360,22 +400,22 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
           if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, bytes);
           if (!GRAD || t.kind == 0) {
             tma_load_2d_pair(a, &p.x_k[gathered], k, m0, bar);
-            tma_load_2d_pair(b, &p.w_k, k, p.col0 + n0, bar);
+            tma_load_2d_pair(b, &p.w_k, k, span.col0 + n0, bar);
           } else if (t.kind == 1) {
             if (p.by_words) {
-              tma_load_2d_pair(a, &p.g_mn, m0, p.prev_col0 + k, bar);
-              tma_load_2d_pair(a + 8192, &p.g_mn, m0 + 64, p.prev_col0 + k, bar);
+              tma_load_2d_pair(a, &p.g_mn[span.shift], m0, span.prev_col0 + k, bar);
+              tma_load_2d_pair(a + 8192, &p.g_mn[span.shift], m0 + 64, span.prev_col0 + k, bar);
             } else {
-              tma_load_2d_pair(a, &p.g_k, k, p.prev_g_row0 + m0, bar);
+              tma_load_2d_pair(a, &p.g_k[span.shift], k, span.prev_g_row0 + m0, bar);
             }
-            tma_load_2d_pair(b, &p.w_mn, n0, p.prev_col0 + k, bar);
-            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, p.prev_col0 + k, bar);
+            tma_load_2d_pair(b, &p.w_mn, n0, span.prev_col0 + k, bar);
+            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, span.prev_col0 + k, bar);
           } else {
             if (p.by_words) {
-              tma_load_2d_pair(a, &p.g_k, k, p.prev_col0 + m0, bar);
+              tma_load_2d_pair(a, &p.g_k[span.shift], k, span.prev_col0 + m0, bar);
             } else {
-              tma_load_2d_pair(a, &p.g_mn, m0, p.prev_g_row0 + k, bar);
-              tma_load_2d_pair(a + 8192, &p.g_mn, m0 + 64, p.prev_g_row0 + k, bar);
+              tma_load_2d_pair(a, &p.g_mn[span.shift], m0, span.prev_g_row0 + k, bar);
+              tma_load_2d_pair(a + 8192, &p.g_mn[span.shift], m0 + 64, span.prev_g_row0 + k, bar);
             }
             tma_load_2d_pair(b, &p.x_mn[gathered], n0, k, bar);
             if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, k, bar);
@@ -494,12 +534,13 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
       } else if (t.kind == 0) {
         const int n0 = t.n * p.block_n;                 // in the piece
         const bool whole = __all_sync(0xffffffffu, row_counts);
-        bf16* g_out = p.g + static_cast<int64_t>(p.g_row0 + m0 + (lane & ~3)) * p.g_pitch + (lane & 3) * 8;
+        bf16* g_out = p.g + static_cast<int64_t>(span.g_row0 + m0 + (lane & ~3)) * span.g_pitch + (lane & 3) * 8;
 #pragma unroll 1
         for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
           const int local = n0 + c;
-          if (local >= p.cols || m0 >= work.row_k * 64) break;   // (kind 2 sums over rows in whole k-blocks)
-          const int col = p.col0 + local;
+          // (in whole k-blocks of the products that sum over columns and over rows)
+          if (local >= (span.cols + 63) / 64 * 64 || m0 >= (rows + 63) / 64 * 64) break;
+          const int col = span.col0 + local;
           uint32_t v[32];
           tmem_ld_32x32(taddr0 + c, v);
           tmem_ld_wait();
@@ -527,23 +568,26 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
 #pragma unroll
             for (int j = 0; j < 32; ++j) g[j] = row_counts ? g[j] : 0.f;
           }
+          if (col + 32 > p.vocab) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = col + j < p.vocab ? g[j] : 0.f;
+          }
           uint4 out[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q)
             out[q] = make_uint4(pack_bf16(g[q * 8], g[q * 8 + 1]), pack_bf16(g[q * 8 + 2], g[q * 8 + 3]), pack_bf16(g[q * 8 + 4], g[q * 8 + 5]),
                                 pack_bf16(g[q * 8 + 6], g[q * 8 + 7]));
           exchange_pieces(out, lane);
-          // (columns behind the piece's last are written, up to its pitch, and never read)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(q) * p.g_pitch + local) = out[q];
+          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(q) * span.g_pitch + local) = out[q];
           if (p.bias_parts != nullptr && m0 < rows) {
             const float s = column_sums(g, lane);
-            if (local + lane < p.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + col + lane] = s;
+            if (local + lane < span.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + col + lane] = s;
           }
         }
       } else if (t.kind == 1) {
         const int n0 = t.n * p.block_h;
-        float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * p.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
+        float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * span.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
 #pragma unroll 1
         for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
           if (n0 + c >= p.hidden || m0 >= rows) break;
@@ -567,18 +611,18 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               float* to = sums + static_cast<int64_t>(q) * p.hidden + col;
-              if (p.prev_first) *reinterpret_cast<uint4*>(to) = out[q]; else red_add_v4(to, out[q]);
+              if (span.prev_col0 == 0) *reinterpret_cast<uint4*>(to) = out[q]; else red_add_v4(to, out[q]);
             }
           }
         }
       } else {
         const int n0 = t.n * p.block_h;
-        const int word = p.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
+        const int word = span.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
         bf16* dw = p.dw + static_cast<int64_t>(word) * p.dw_stride + (lane & 3) * 8;
 #pragma unroll 1
         for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
           const int col = n0 + c;
-          if (col >= p.hidden || p.prev_col0 + m0 >= p.vocab) break;
+          if (col >= p.hidden || span.prev_col0 + m0 >= p.vocab) break;
           uint32_t v[32];
           if (t.k_blocks > 0) {
             tmem_ld_32x32(taddr0 + c, v);
@@ -588,7 +632,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
             for (int j = 0; j < 32; ++j) v[j] = 0u;
           }
           if (p.accumulate) {
-            const int mine = p.prev_col0 + row;
+            const int mine = span.prev_col0 + row;
             const bf16* old = p.dw + static_cast<int64_t>(mine) * p.dw_stride + col;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {               // (hidden is a multiple of eight)
@@ -903,6 +947,31 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
 
 constexpr int kRowsThreads = 256;
 
+// Ranges of the vocabulary that dx of a piece is summed over in: a tile of it should be no longer than half of what a pair has to do
+// in the launch (a tile counts as at least six k-blocks: its epilogue).
+__host__ __device__ inline int choose_ranges(int rows, int piece, int pieces, int hidden, int block_h) {
+  const int64_t m = (rows + kTile - 1) / kTile, h = (hidden + block_h - 1) / block_h, v = (piece + kTile - 1) / kTile;
+  const int k1 = (piece + 63) / 64, k2 = (rows + 63) / 64, k0 = (hidden + 63) / 64;
+  const int64_t all = m * h * k1 + v * h * (k2 > 6 ? k2 : 6) + (pieces > 1 ? m * v * (k0 > 6 ? k0 : 6) : 0);
+  int64_t longest = all / 74 / 2;
+  if (longest < 8) longest = 8;
+  const int64_t ranges = (k1 + longest - 1) / longest;
+  return ranges < kMaxRanges ? static_cast<int>(ranges) : kMaxRanges;
+}
+
+// The cut for `rows` rows: pieces as wide as the buffers hold for so many, as few ranges as keep the pairs busy.
+__device__ inline void make_plan(const VocabRowsParams& p, int rows) {
+  VocabPlan plan;
+  plan.rows = rows;
+  plan.row_pitch = max(1, (rows + kTile - 1) / kTile) * kTile;
+  plan.shift = 0;
+  while (plan.shift < p.max_shift && (p.buffer_rows >> (plan.shift + 1)) >= plan.row_pitch) ++plan.shift;
+  plan.piece = p.piece << plan.shift;
+  plan.pieces = (p.vocab + plan.piece - 1) / plan.piece;
+  plan.ranges = min(choose_ranges(rows, min(plan.piece, p.vocab), plan.pieces, p.hidden, p.block_h), p.dx_rows / plan.row_pitch);
+  *p.plan = plan;
+}
+
 // A CTA per `rows_per_cta` rows counts the labels before them and all of them (a few KB that stay in L2), and gives every row with a
 // label its place.  Unless all rows have one, their hidden states are gathered, with zeros up to the next k-block of the products that
 // sum over rows.
@@ -919,7 +988,7 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
   if (tid == 0) s_before = s_all = 0;
   __syncthreads();
   int before = 0, all = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int r = tid; r < p.rows; r += kRowsThreads) {
     const int has = has_label(r) ? 1 : 0;
     all += has;
@@ -937,7 +1006,10 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
   __syncthreads();
   all = s_all;
   if (blockIdx.x == 0) {
-    if (tid == 0) *p.count = all;
+    if (tid == 0) {
+      *p.count = all;
+      if (p.plan != nullptr) make_plan(p, all);
+    }
     for (int i = tid; i < p.n_counters; i += kRowsThreads) p.counters[i] = 0;
   }
   const int vectors = p.hidden / 8;
@@ -1038,6 +1110,8 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_con
   grid_launch_dependents();
   const int lane = threadIdx.x & 31;
   const int blocks = (p.hidden + 255) / 256;
+  const int ranges = p.plan != nullptr ? p.plan->ranges : p.ranges;
+  const int64_t row_pitch = p.plan != nullptr ? p.plan->row_pitch : p.row_pitch;
   const int64_t step = static_cast<int64_t>(gridDim.x) * (kJoinThreads / 32), units = static_cast<int64_t>(p.rows) * blocks;
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); u < units; u += step) {
     const int row = static_cast<int>(u / blocks), c = static_cast<int>(u % blocks) * 256 + lane * 8;
@@ -1051,8 +1125,8 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_con
       const uint4 word = __ldg(reinterpret_cast<const uint4*>(p.w + static_cast<int64_t>(label) * p.w_stride + c));
       const float residual = p.row_residual[place];
 #pragma unroll 8
-      for (int s = 0; s < p.ranges; ++s) {
-        const float4* f = reinterpret_cast<const float4*>(src + static_cast<int64_t>(s) * p.row_pitch * p.hidden);
+      for (int s = 0; s < ranges; ++s) {
+        const float4* f = reinterpret_cast<const float4*>(src + s * row_pitch * p.hidden);
         const float4 x = f[0], w = f[1];
         a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
         b.x += w.x; b.y += w.y; b.z += w.z; b.w += w.w;
@@ -1125,9 +1199,8 @@ size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 constexpr int kGatherRows = kTile;       // up to one tile of rows costs the same however few of them count
 constexpr int kFewPartCtas = 256;        // place for the CTAs of the kernel for few rows
-constexpr int64_t kPieceElements = 32 << 20;   // of g of one piece: 64 MB
+constexpr int64_t kPieceElements = 64 << 20;   // of g of one piece: 128 MB
 constexpr int kMinPiece = 2048;
-constexpr int kMaxRanges = 32;
 
 struct ForwardPlan {
   int block_n, tiles_n, part_pitch;
@@ -1166,15 +1239,14 @@ ForwardPlan forward_plan(int rows, int vocab, int hidden, int sm_count) {
 }
 
 struct GradPlan {
-  int piece, pieces, buffers, block_h, ranges, g_pitch;
+  int piece, pieces, buffers, block_h, ranges, g_pitch, max_shift;
   bool few;
-  int64_t row_pitch;
-  size_t count, counters, row_of, row_label, row_lse, row_weight, row_residual, place_of, gathered, g, dx, bias_parts, bytes;
+  int64_t row_pitch, dx_rows;
+  size_t count, plan, counters, row_of, row_label, row_lse, row_weight, row_residual, place_of, gathered, g, dx, bias_parts, bytes;
 };
 GradPlan grad_plan(int rows, int vocab, int hidden) {
   GradPlan f;
   f.row_pitch = static_cast<int64_t>(ceil_div(rows, kTile)) * kTile;
-  const int m = static_cast<int>(f.row_pitch / kTile);
   const int64_t all = static_cast<int64_t>(ceil_div(vocab, kTile)) * kTile;
   f.few = rows <= kFewRows;
   f.g_pitch = (rows + 63) / 64 * 64;       // (few rows: g is kept by words)
@@ -1186,19 +1258,15 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.pieces = ceil_div(all, f.piece);
   f.buffers = f.pieces > 1 ? 2 : 1;
   f.block_h = hidden > kHalf ? kTile : kHalf;
-  // Ranges of the vocabulary that dx of a piece is summed over in: a tile of it should be no longer than half of what a pair has to do
-  // in the launch (a tile counts as at least six k-blocks: its epilogue).
-  const int h = ceil_div(hidden, f.block_h);
-  const int k1 = f.piece / 64, k2 = ceil_div(rows, 64), k0 = ceil_div(hidden, 64);
-  const int64_t all_k = static_cast<int64_t>(m) * h * k1 + static_cast<int64_t>(f.piece / kTile) * h * (k2 > 6 ? k2 : 6) +
-                        (f.pieces > 1 ? static_cast<int64_t>(m) * (f.piece / kTile) * (k0 > 6 ? k0 : 6) : 0);
-  int64_t longest = all_k / 74 / 2;
-  if (longest < 8) longest = 8;
-  f.ranges = ceil_div(k1, longest);
-  if (f.ranges > kMaxRanges) f.ranges = kMaxRanges;
+  f.max_shift = 0;
+  while (!f.few && f.max_shift + 1 < kVocabShifts && (static_cast<int64_t>(f.piece) << f.max_shift) < all && (f.row_pitch >> (f.max_shift + 1)) >= kTile)
+    ++f.max_shift;
+  f.ranges = choose_ranges(rows, f.piece, f.pieces, hidden, f.block_h);
+  f.dx_rows = f.row_pitch * (f.max_shift > 0 && f.ranges < 2 ? 2 : f.ranges);   // (fewer rows with a label: more ranges)
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += whole_lines(bytes); return here; };
   f.count = take(256);
+  f.plan = take(sizeof(VocabPlan));
   f.counters = take((static_cast<size_t>(f.pieces) + 1) * 4);
   f.row_of = take(f.row_pitch * 4);
   f.row_label = take(f.row_pitch * 4);
@@ -1208,7 +1276,7 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.place_of = take(f.row_pitch * 4);
   f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
   f.g = take(static_cast<size_t>(f.buffers) * (f.few ? f.g_pitch : f.row_pitch) * f.piece * 2);
-  f.dx = take(static_cast<size_t>(f.ranges) * f.row_pitch * hidden * 4);
+  f.dx = take(static_cast<size_t>(f.dx_rows) * hidden * 4);
   f.bias_parts = take(f.few ? 0 : static_cast<size_t>(f.row_pitch / 32) * vocab * 4);
   f.bytes = at;
   return f;
@@ -1258,7 +1326,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
   }
   VocabLossParams p;
   memset(&p, 0, sizeof(p));
-  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.cols = c.vocab; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
   p.labels = f.gather ? at<int32_t>(ws, f.row_label) : c.labels;
   p.count = f.gather ? at<int32_t>(ws, f.count) : nullptr;
   p.label_logit = at<float>(ws, f.label_logit); p.parts = at<float2>(ws, f.parts); p.part_pitch = f.part_pitch; p.status = c.status;
@@ -1296,7 +1364,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   VocabLossParams p;
   memset(&p, 0, sizeof(p));
   p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias; p.status = c.status;
-  p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.dx_sums = at<float>(ws, f.dx);
+  p.dx_sums = at<float>(ws, f.dx);
   p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate;
   p.dw = c.dw; p.dw_stride = c.dw_stride;
   if ((e = encode_matrix_map(&p.w_mn, c.w, c.vocab, c.hidden, c.w_stride * 2, 64, 64, false)) != cudaSuccess) return e;
@@ -1314,13 +1382,13 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     int ctas = 0;
     if ((e = launch_few<true>(w, sm_count, &ctas, stream)) != cudaSuccess || !products) return e;
     const int words = ceil_div(c.vocab, 128) * 128;
-    if ((e = encode_matrix_map(&p.g_k, g, words, f.g_pitch, f.g_pitch * 2, kHalf, 64, false)) != cudaSuccess ||
-        (e = encode_matrix_map(&p.g_mn, g, words, f.g_pitch, f.g_pitch * 2, 64, 64, false)) != cudaSuccess ||
+    if ((e = encode_matrix_map(&p.g_k[0], g, words, f.g_pitch, f.g_pitch * 2, kHalf, 64, false)) != cudaSuccess ||
+        (e = encode_matrix_map(&p.g_mn[0], g, words, f.g_pitch, f.g_pitch * 2, 64, 64, false)) != cudaSuccess ||
         (e = encode_matrix_map(&p.x_mn[0], gathered, f.g_pitch, c.hidden, h_stride, 64, 64, false)) != cudaSuccess)
       return e;
     p.x_mn[1] = p.x_mn[0];
     p.x_k[0] = p.w_k = p.w_mn;      // (of kind 0, which has no tiles here)
-    p.by_words = 1; p.prev_cols = c.vocab; p.prev_first = 1; p.counter = w.counter;
+    p.by_words = 1; p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.counter = w.counter;
     const int tiles = row_tiles * hidden_tiles * f.ranges + ceil_div(c.vocab, kTile) * hidden_tiles;
     if ((e = launch_pairs<true>(p, tiles, sm_count, stream)) != cudaSuccess || c.dx == nullptr) return e;
     return launch_kernel(vocab_dx_kernel, dx_ctas, dim3(kJoinThreads), 0, stream, d);
@@ -1333,37 +1401,32 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   r.row_lse = at<float>(ws, f.row_lse); r.row_weight = at<float>(ws, f.row_weight); r.place_of = at<int32_t>(ws, f.place_of);
   r.lse = c.lse; r.grad_loss = c.grad_loss; r.gathered = at<bf16>(ws, f.gathered);
   r.counters = at<uint32_t>(ws, f.counters); r.n_counters = f.pieces + 1; r.status = c.status;
+  r.plan = at<VocabPlan>(ws, f.plan); r.piece = f.piece; r.max_shift = f.max_shift; r.buffer_rows = static_cast<int>(f.row_pitch);
+  r.dx_rows = static_cast<int>(f.dx_rows); r.block_h = f.block_h;
   int ctas = 0;
   launch_rows_setup(&r, &ctas);
   if ((e = launch_kernel(vocab_rows_kernel, dim3(ctas), dim3(kRowsThreads), 0, stream, r)) != cudaSuccess) return e;
 
-  p.labels = r.row_label; p.count = r.count; p.row_lse = r.row_lse; p.row_weight = r.row_weight; p.row_residual = at<float>(ws, f.row_residual);
+  p.labels = r.row_label; p.plan = r.plan; p.row_lse = r.row_lse; p.row_weight = r.row_weight; p.row_residual = at<float>(ws, f.row_residual);
   p.bias_parts = c.db != nullptr ? at<float>(ws, f.bias_parts) : nullptr; p.bias_pitch = c.vocab;
-  p.g = g; p.g_pitch = f.piece;
-  const int64_t g_rows = f.buffers * f.row_pitch, g_stride = static_cast<int64_t>(f.piece) * 2;
+  p.g = g; p.buffers = f.buffers; p.buffer_rows = static_cast<int>(f.row_pitch);
   if ((e = encode_matrix_map(&p.x_k[0], c.x, c.rows, c.hidden, c.x_stride * 2, kHalf, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_k[1], gathered, f.row_pitch, c.hidden, h_stride, kHalf, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_mn[0], c.x, c.rows, c.hidden, c.x_stride * 2, 64, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_mn[1], gathered, f.row_pitch, c.hidden, h_stride, 64, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, kHalf, 64, false)) != cudaSuccess)
     return e;
-  for (int j = 0; j <= f.pieces; ++j) {
-    if (j == f.pieces && !products) break;
-    p.col0 = j * f.piece;
-    p.cols = j < f.pieces ? (c.vocab - p.col0 < f.piece ? c.vocab - p.col0 : f.piece) : 0;
-    p.g_row0 = (j & (f.buffers - 1)) * static_cast<int>(f.row_pitch);
-    p.prev_col0 = (j - 1) * f.piece;
-    p.prev_cols = j > 0 ? (c.vocab - p.prev_col0 < f.piece ? c.vocab - p.prev_col0 : f.piece) : 0;
-    p.prev_g_row0 = j > 0 ? ((j - 1) & (f.buffers - 1)) * static_cast<int>(f.row_pitch) : 0;
-    p.prev_first = j == 1 ? 1 : 0;
-    p.counter = r.counters + j;
-    // (columns behind the piece's last one are neither stored nor read: the products over the vocabulary see zeros there)
-    if (p.prev_cols > 0 && ((e = encode_matrix_map(&p.g_k, g, g_rows, p.prev_cols, g_stride, kHalf, 64, false)) != cudaSuccess ||
-                            (e = encode_matrix_map(&p.g_mn, g, g_rows, p.prev_cols, g_stride, 64, 64, false)) != cudaSuccess))
+  for (int k = 0; k <= f.max_shift; ++k) {
+    const int64_t g_rows = f.buffers * f.row_pitch >> k, g_cols = static_cast<int64_t>(f.piece) << k;
+    if ((e = encode_matrix_map(&p.g_k[k], g, g_rows, g_cols, g_cols * 2, kHalf, 64, false)) != cudaSuccess ||
+        (e = encode_matrix_map(&p.g_mn[k], g, g_rows, g_cols, g_cols * 2, 64, 64, false)) != cudaSuccess)
       return e;
-    const int64_t tiles = static_cast<int64_t>(row_tiles) * ceil_div(p.cols, kTile) +
-                          (p.prev_cols > 0 ? static_cast<int64_t>(row_tiles) * hidden_tiles * f.ranges + static_cast<int64_t>(ceil_div(p.prev_cols, kTile)) * hidden_tiles : 0);
-    if ((e = launch_pairs<true>(p, static_cast<int>(tiles < (1 << 30) ? tiles : 1 << 30), sm_count, stream)) != cudaSuccess) return e;
+  }
+  // (sized for all rows; with fewer, the pieces are wider and the last launches find nothing to do)
+  for (int j = 0; j <= f.pieces && (j < f.pieces || products); ++j) {
+    p.index = j;
+    p.counter = r.counters + j;
+    if ((e = launch_pairs<true>(p, sm_count, sm_count, stream)) != cudaSuccess) return e;
   }
   if (c.db != nullptr) {
     VocabBiasParams b;
@@ -1372,7 +1435,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     if ((e = launch_kernel(vocab_bias_kernel, dim3(ceil_div(c.vocab, 32)), dim3(256), 0, stream, b)) != cudaSuccess) return e;
   }
   if (c.dx == nullptr) return cudaSuccess;
-  d.place_of = r.place_of;
+  d.place_of = r.place_of; d.plan = r.plan;
   return launch_kernel(vocab_dx_kernel, dx_ctas, dim3(kJoinThreads), 0, stream, d);
 }
 
