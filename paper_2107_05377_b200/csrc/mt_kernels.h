@@ -472,24 +472,30 @@ size_t vocab_loss_grad_workspace(int rows, int vocab, int hidden);
 cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t stream);
 cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStream_t stream);
 
-// How a gradient is cut up, decided on the device from the number of rows with a label.
-struct VocabPlan {
-  int32_t rows;                // with a label
+// What one launch of a gradient works on, decided on the device from the number of rows with a label (64 bytes, loaded as such).
+struct alignas(16) VocabWork {
+  int32_t rows;                // in use
+  int32_t col0, cols;          // columns of the vocabulary whose g is taken
+  int32_t prev_col0, prev_cols;   // columns whose g is taken into the products
+  int32_t g_row0, prev_g_row0; // first row of their buffers of g
   int32_t shift;               // pieces are this many powers of two wider than for all rows
-  int32_t piece, pieces;       // columns of a piece of the vocabulary, and how many there are
+  int32_t row_tiles;           // tiles of 256 rows
+  int32_t n0, n1, n2;          // tiles of each kind
+  int32_t k1, k2;              // k-blocks of kinds 1 (one range of the vocabulary) and 2
   int32_t ranges;              // of a piece, that dx is summed over in
   int32_t row_pitch;           // rows in whole tiles
 };
+static_assert(sizeof(VocabWork) == 64, "loaded as four vectors");
 constexpr int kVocabShifts = 4;
 // The products.  Index 1 of the maps of x: the rows with a label, gathered.  Boxes of 128 x 64 (block_n / 2 x 64) for operands along K,
 // 64 x 64 for operands whose rows run along K.
 struct VocabLossParams {
-  CUtensorMap x_k[2], w_k, x_mn[2], w_mn, g_k[kVocabShifts], g_mn[kVocabShifts];   // (g: by VocabPlan::shift)
+  CUtensorMap x_k[2], w_k, x_mn[2], w_mn, g_k[kVocabShifts], g_mn[kVocabShifts];   // (g: by VocabWork::shift)
   const bf16* bias;
   const int32_t* labels;       // of the rows in use
   const int32_t* count;        // forward: rows in use (or null: rows)
-  const VocabPlan* plan;       // backward (null: few rows, and what follows is given)
-  const float* row_lse;
+  const VocabWork* work;       // backward, of this launch (null: few rows, all of it as given below)
+  const float* row_shift;      // backward: log2 |weight| - lse log2 e
   const float* row_weight;
   float* row_residual;         // backward: what rounding takes from the label's entry of g
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
@@ -502,9 +508,9 @@ struct VocabLossParams {
   uint32_t* counter;           // next tile to hand out
   uint32_t* status;
   int32_t rows, vocab, hidden, block_n, block_h;
-  int32_t index;               // backward: of the launch: g of this piece, the products of the one before
-  int32_t buffers, buffer_rows;   // of g, at shift 0
-  int32_t row_pitch, ranges;   // (few rows)
+  int32_t piece;               // backward: columns of g's buffers at shift 0
+  int32_t n_tiles;             // of a product's columns: forward of the vocabulary, backward of the hidden size
+  int32_t row_pitch, ranges, range_blocks;   // (few rows; k-blocks of a range)
   int32_t part_pitch, bias_pitch;
   int32_t want_x, want_w, accumulate;
   int32_t by_words;            // g lies by words, [vocab][rows] (few rows; g_k: boxes of 128 words, g_mn: of 64)
@@ -536,15 +542,15 @@ struct VocabRowsParams {
   const float* grad_loss;
   int64_t x_stride;
   int32_t rows, vocab, hidden, rows_per_cta, n_counters;
-  VocabPlan* plan;             // backward; or null.  From what there is place for:
-  int32_t piece, max_shift, buffer_rows, dx_rows, block_h;
+  VocabWork* work;             // backward: of n_counters launches; or null.  From what there is place for:
+  int32_t piece, max_shift, buffers, buffer_rows, dx_rows, block_h, want_x, want_w;
   int32_t* count;
   uint32_t* counters;          // set to zero
   int32_t* row_of;             // caller's row of a row in use
   int32_t* place_of;           // the other way round (-1: none), or null
   int32_t* row_label;
-  float* row_lse;              // or null
-  float* row_weight;           // or null
+  float* row_shift;            // backward: see VocabLossParams
+  float* row_weight;
   bf16* gathered;
   float* loss_out;             // forward: zeros for rows without a label
   float* lse_out;
@@ -561,23 +567,21 @@ struct VocabJoinParams {
   int32_t rows, vocab, part_pitch, n_parts;
   uint32_t* status;
 };
-struct VocabDxParams {
-  const VocabPlan* plan;       // (null: ranges and row_pitch as given)
+struct VocabFinishParams {
+  const VocabWork* work;       // (null: few rows, in place, ranges and row_pitch as given)
   const float* sums;           // [ranges][row_pitch][hidden]
-  const int32_t* place_of;     // or null: in place
+  const int32_t* place_of;
   const int32_t* labels;
   const float* row_residual;
   const bf16* w;
   int64_t w_stride;
-  bf16* dx;
+  bf16* dx;                    // or null
   int64_t dx_stride, row_pitch;
   int32_t rows, vocab, hidden, ranges;
-};
-struct VocabBiasParams {
-  const float* parts;
-  const int32_t* count;
-  float* out;
-  int32_t rows, cols, pitch, accumulate;
+  int32_t db_ctas;             // CTAs that take db, the first of the grid
+  const float* bias_parts;     // [block of 32 rows][vocab]
+  float* db;                   // or null
+  int32_t accumulate;
 };
 
 }  // namespace mt

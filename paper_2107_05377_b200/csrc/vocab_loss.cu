@@ -101,133 +101,116 @@ __device__ __forceinline__ void send_words(uint32_t cluster_addr, int a, int b, 
                : "memory");
 }
 
-// What a launch works on.
-struct Span {
-  int rows;                    // in use
-  int col0, cols;              // columns of the vocabulary whose logits are taken
-  int prev_col0, prev_cols;    // (backward) columns whose g is taken into the products
-  int g_row0, prev_g_row0;     // first row of their buffers of g
-  int g_pitch, shift;
-  int ranges, row_pitch;
-};
+// What a launch works on: the forward pass and few rows from the arguments, otherwise as the rows' kernel has left it (without a division
+// here: every clock before the first copy counts in a short launch).
 template <bool GRAD>
-__device__ __forceinline__ Span make_span(const VocabLossParams& p) {
-  Span s = {};
-  if (!GRAD) {
-    s.rows = p.count != nullptr ? min(p.rows, *reinterpret_cast<const volatile int*>(p.count)) : p.rows;
-    s.cols = p.vocab;
-  } else if (p.plan == nullptr) {
-    s.rows = p.rows;
-    s.prev_cols = p.vocab;
-    s.ranges = p.ranges;
-    s.row_pitch = p.row_pitch;
-  } else {
-    const volatile VocabPlan* plan = p.plan;
-    s.rows = plan->rows;
-    s.shift = plan->shift;
-    s.ranges = plan->ranges;
-    s.row_pitch = plan->row_pitch;
-    s.g_pitch = plan->piece;
-    const int pieces = plan->pieces;
-    if (p.index < pieces) {
-      s.col0 = p.index * s.g_pitch;
-      s.cols = min(s.g_pitch, p.vocab - s.col0);
-      s.g_row0 = (p.index & (p.buffers - 1)) * (p.buffer_rows >> s.shift);
-    }
-    if (p.index > 0 && p.index <= pieces) {
-      s.prev_col0 = (p.index - 1) * s.g_pitch;
-      s.prev_cols = min(s.g_pitch, p.vocab - s.prev_col0);
-      s.prev_g_row0 = ((p.index - 1) & (p.buffers - 1)) * (p.buffer_rows >> s.shift);
-    }
+__device__ __forceinline__ VocabWork load_work(const VocabLossParams& p) {
+  VocabWork w;
+  if (GRAD && p.work != nullptr) {
+    const int4* src = reinterpret_cast<const int4*>(p.work);
+    int4* dst = reinterpret_cast<int4*>(&w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = __ldcg(src + i);
+    return w;
   }
-  return s;
-}
-
-// The tiles of a launch, in the order in which they are handed out: long ones first.
-struct Work {
-  int row_tiles;               // 256 rows each
-  int n0, n1, n2;              // tiles of each kind
-  int k0, k1, k2;              // their k-blocks (k1: of one range of the vocabulary)
-  bool first1;                 // kind 1 before kind 2
-  int hidden_tiles;
-};
-struct Tile {
-  int kind, m, n, range, k_blocks, k_begin;
-};
-
-template <bool GRAD>
-__device__ __forceinline__ Work make_work(const VocabLossParams& p, const Span& s) {
-  Work w;
-  w.row_tiles = (s.rows + kTile - 1) / kTile;
-  w.n0 = w.row_tiles * ((s.cols + p.block_n - 1) / p.block_n);
-  w.k0 = (p.hidden + 63) / 64;
-  w.n1 = w.n2 = w.k1 = w.k2 = 0;
-  w.first1 = false;
-  w.hidden_tiles = 1;
-  if (GRAD) {
-    w.hidden_tiles = (p.hidden + p.block_h - 1) / p.block_h;
-    if (s.prev_cols > 0) {
-      if (p.want_x) w.n1 = w.row_tiles * w.hidden_tiles * s.ranges;
-      if (p.want_w) w.n2 = (s.prev_cols + kTile - 1) / kTile * w.hidden_tiles;
-      w.k1 = ((s.prev_cols + 63) / 64 + s.ranges - 1) / s.ranges;
-      w.k2 = (s.rows + 63) / 64;
-      w.first1 = w.k1 > w.k2;
-    }
+  w = VocabWork{};
+  w.rows = !GRAD && p.count != nullptr ? min(p.rows, __ldcg(p.count)) : p.rows;
+  w.row_tiles = (w.rows + kTile - 1) / kTile;
+  if (!GRAD) {
+    w.cols = p.vocab;
+    w.n0 = w.row_tiles * p.n_tiles;
+  } else {
+    w.prev_cols = p.vocab;
+    w.ranges = p.ranges;
+    w.row_pitch = p.row_pitch;
+    w.n1 = p.want_x ? p.n_tiles * p.ranges : 0;             // (one tile of rows)
+    w.n2 = p.want_w ? (p.vocab + kTile - 1) / kTile * p.n_tiles : 0;
+    w.k1 = p.range_blocks;
+    w.k2 = (w.rows + 63) / 64;
   }
   return w;
 }
+
+// i / d by a reciprocal of d.
+__device__ __forceinline__ int divide(int i, int d, float rcp) {
+  if (i >= 1 << 22) return i / d;
+  int q = static_cast<int>(static_cast<float>(i) * rcp);
+  const int r = i - q * d;
+  if (r < 0) --q;
+  if (r >= d) ++q;
+  return q;
+}
+
+struct Tile {
+  int kind, m, n, range, k_blocks, k_begin;
+};
+// The tiles of a launch in the order in which they are handed out, long ones first.  n_tiles: of the columns of a matrix product (forward:
+// the vocabulary; backward, kinds 1 and 2: the hidden size).
 template <bool GRAD>
-__device__ __forceinline__ Tile find_tile(const Span& s, const Work& w, int i) {
+__device__ __forceinline__ Tile find_tile(const VocabWork& w, int n_tiles, int k0, int i) {
   Tile t;
   t.range = 0;
   t.k_begin = 0;
   if (GRAD && i < w.n1 + w.n2) {
-    const bool is1 = w.first1 ? i < w.n1 : i >= w.n2;
+    const bool first1 = w.k1 > w.k2;
+    const bool is1 = first1 ? i < w.n1 : i >= w.n2;
+    const float rcp_n = __frcp_rn(static_cast<float>(n_tiles));
     if (is1) {
-      if (!w.first1) i -= w.n2;
+      if (!first1) i -= w.n2;
       t.kind = 1;
-      t.m = i % w.row_tiles;
-      i /= w.row_tiles;
-      t.n = i % w.hidden_tiles;
-      t.range = i / w.hidden_tiles;
+      const int q = divide(i, w.row_tiles, __frcp_rn(static_cast<float>(w.row_tiles)));
+      t.m = i - q * w.row_tiles;
+      t.range = divide(q, n_tiles, rcp_n);
+      t.n = q - t.range * n_tiles;
       t.k_begin = t.range * w.k1;
-      const int all = (s.prev_cols + 63) / 64;
-      t.k_blocks = all - t.k_begin < w.k1 ? (all > t.k_begin ? all - t.k_begin : 0) : w.k1;
+      const int all = (w.prev_cols + 63) / 64;
+      t.k_blocks = max(0, min(w.k1, all - t.k_begin));
     } else {
-      if (w.first1) i -= w.n1;
+      if (first1) i -= w.n1;
       t.kind = 2;
-      const int m_tiles = w.n2 / w.hidden_tiles;
-      t.m = i % m_tiles;
-      t.n = i / m_tiles;
+      const int m_tiles = (w.prev_cols + kTile - 1) / kTile;
+      t.n = divide(i, m_tiles, __frcp_rn(static_cast<float>(m_tiles)));
+      t.m = i - t.n * m_tiles;
       t.k_blocks = w.k2;
     }
     return t;
   }
   i -= w.n1 + w.n2;
   t.kind = 0;
-  t.m = i % w.row_tiles;
-  t.n = i / w.row_tiles;
-  t.k_blocks = w.k0;
+  t.n = divide(i, w.row_tiles, __frcp_rn(static_cast<float>(w.row_tiles)));
+  t.m = i - t.n * w.row_tiles;
+  t.k_blocks = k0;
   return t;
 }
 
-// Bias of 32 columns from `col` on (0 where there is none).
-__device__ __forceinline__ void add_bias(const bf16* bias, int col, int vocab, float (&z)[32]) {
+// Bias of 32 columns from `col` on, asked for before the accumulator is waited for, and added after.
+struct Bias32 { uint4 v[4]; };
+__device__ __forceinline__ void load_bias(const bf16* bias, int col, int vocab, Bias32& b) {
   if (bias == nullptr) return;
   if (col + 32 <= vocab) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint4 b = __ldg(reinterpret_cast<const uint4*>(bias + col) + q);
-      const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        z[q * 8 + 2 * j] += bf16_lo(w[j]);
-        z[q * 8 + 2 * j + 1] += bf16_hi(w[j]);
-      }
-    }
+    for (int q = 0; q < 4; ++q) b.v[q] = __ldg(reinterpret_cast<const uint4*>(bias + col) + q);
   } else {
+    uint32_t w[16];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) if (col + j < vocab) z[j] += __bfloat162float(bias[col + j]);
+    for (int j = 0; j < 32; ++j) {
+      const uint32_t x = col + j < vocab ? __bfloat16_as_ushort(bias[col + j]) : 0u;
+      w[j / 2] = j % 2 ? w[j / 2] | (x << 16) : x;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) b.v[q] = make_uint4(w[q * 4], w[q * 4 + 1], w[q * 4 + 2], w[q * 4 + 3]);
+  }
+}
+__device__ __forceinline__ void add_bias(const bf16* bias, const Bias32& b, float (&z)[32]) {
+  if (bias == nullptr) return;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t w[4] = {b.v[q].x, b.v[q].y, b.v[q].z, b.v[q].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      z[q * 8 + 2 * j] += bf16_lo(w[j]);
+      z[q * 8 + 2 * j + 1] += bf16_hi(w[j]);
+    }
   }
 }
 
@@ -308,28 +291,27 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
       prefetch_tensormap(&p.x_mn[0]);
     }
   }
-  // (a first look at each line of the arguments costs some hundred clocks: before the wait, not after)
-  asm volatile("" ::"r"(p.rows), "r"(p.block_n), "r"(p.block_h), "r"(p.index), "r"(p.want_w),
-               "l"(p.labels), "l"(p.counter));
+  // What the arguments alone decide is computed before the wait (a first look at each line of them costs some hundred clocks).
+  const bool given = GRAD ? p.work == nullptr : p.count == nullptr;
+  VocabWork work = {};
+  if (given) work = load_work<GRAD>(p);
+  asm volatile("" ::"r"(p.rows), "r"(p.block_n), "r"(p.block_h), "r"(p.n_tiles), "r"(p.want_w), "l"(p.labels), "l"(p.counter));
   grid_dependency_wait();
   grid_launch_dependents();
-  const Span span = make_span<GRAD>(p);
-  const int rows = span.rows;
+  if (!given) work = load_work<GRAD>(p);
+  const int rows = work.rows, g_pitch = p.piece << work.shift;
   const int gathered = rows == p.rows ? 0 : 1;      // which x: the caller's, or the rows with a label
-  const Work work = make_work<GRAD>(p, span);
   const int total = work.n0 + work.n1 + work.n2;
+  const int k0 = (p.hidden + 63) / 64;
 
-  // Tiles.  Forward: worker, worker + n_workers, ... (all tiles cost the same).  Backward: the next of the list, whoever is free first;
-  // rank 0's producer takes them from a counter in memory and announces them to all roles of both CTAs.  (Which pair computes a tile
-  // has no influence on it.)
+  // Tiles.  Forward: worker, worker + n_workers, ... (all tiles cost the same).  Backward: the first one likewise, then the next of the
+  // list, whoever is free first; rank 0's producer takes them from a counter in memory and announces them to all roles of both CTAs.
+  // (Which pair computes a tile has no influence on it.)
   int slot = 0;
   uint32_t slot_phase = 0;
+  Tile t = find_tile<GRAD>(work, p.n_tiles, k0, worker);
   // Forward: m and n of the next tile of this worker without a division per tile.
   const int step_m = n_workers % max(work.row_tiles, 1), step_n = n_workers / max(work.row_tiles, 1);
-  Tile t;
-  t.kind = 0; t.range = 0; t.k_begin = 0; t.k_blocks = work.k0;
-  t.m = worker % max(work.row_tiles, 1);
-  t.n = worker / max(work.row_tiles, 1);
   int at_tile = worker;
   auto next_static = [&](bool first) -> bool {
     if (!first) {
@@ -341,7 +323,8 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
     return at_tile < total;
   };
   // Backward, the roles other than rank 0's producer: the next tile; false at the end and when the CTA is giving up.
-  auto next_announced = [&]() -> bool {
+  auto next_announced = [&](bool first) -> bool {
+    if (first) return worker < total;
     if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_full + 8 * slot, slot_phase, abort_flag))) return false;
     t.kind = slot_tile[slot].x;
     t.m = slot_tile[slot].y;
@@ -366,9 +349,11 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
     // (backward, rank 0) The tile after the one whose copies are under way is asked for when its turn begins and announced some k-blocks
     // later, so that neither the trip to the counter nor that to the other CTA holds up a copy.
     int asked = 0;
+    if (GRAD && rank == 0 && lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
     Tile ahead = t;
+    if (worker >= total) ahead.kind = -1;
     auto announce = [&](int i) -> bool {
-      if (i < total) ahead = find_tile<GRAD>(span, work, i); else ahead.kind = -1;
+      if (i < total) ahead = find_tile<GRAD>(work, p.n_tiles, k0, i); else ahead.kind = -1;
       if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) return false;
       if (lane < 2)
         send_words(map_to_cta(smem_u32(const_cast<int4*>(slot_tile) + slot), lane), ahead.kind, ahead.m, ahead.n | (ahead.range << 16), ahead.k_blocks,
@@ -378,12 +363,11 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
       if (ahead.kind >= 0 && lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
       return true;
     };
-    if (GRAD && rank == 0) ok = announce(worker);
     for (bool first = true; ok; first = false) {
       if (!GRAD) {
         if (!next_static(first)) break;
       } else if (rank != 0) {
-        if (!next_announced()) break;
+        if (!next_announced(first)) break;
       } else {
         t = ahead;
         if (t.kind < 0) break;
@@ -400,22 +384,22 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
           if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, bytes);
           if (!GRAD || t.kind == 0) {
             tma_load_2d_pair(a, &p.x_k[gathered], k, m0, bar);
-            tma_load_2d_pair(b, &p.w_k, k, span.col0 + n0, bar);
+            tma_load_2d_pair(b, &p.w_k, k, work.col0 + n0, bar);
           } else if (t.kind == 1) {
             if (p.by_words) {
-              tma_load_2d_pair(a, &p.g_mn[span.shift], m0, span.prev_col0 + k, bar);
-              tma_load_2d_pair(a + 8192, &p.g_mn[span.shift], m0 + 64, span.prev_col0 + k, bar);
+              tma_load_2d_pair(a, &p.g_mn[work.shift], m0, work.prev_col0 + k, bar);
+              tma_load_2d_pair(a + 8192, &p.g_mn[work.shift], m0 + 64, work.prev_col0 + k, bar);
             } else {
-              tma_load_2d_pair(a, &p.g_k[span.shift], k, span.prev_g_row0 + m0, bar);
+              tma_load_2d_pair(a, &p.g_k[work.shift], k, work.prev_g_row0 + m0, bar);
             }
-            tma_load_2d_pair(b, &p.w_mn, n0, span.prev_col0 + k, bar);
-            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, span.prev_col0 + k, bar);
+            tma_load_2d_pair(b, &p.w_mn, n0, work.prev_col0 + k, bar);
+            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, work.prev_col0 + k, bar);
           } else {
             if (p.by_words) {
-              tma_load_2d_pair(a, &p.g_k[span.shift], k, span.prev_col0 + m0, bar);
+              tma_load_2d_pair(a, &p.g_k[work.shift], k, work.prev_col0 + m0, bar);
             } else {
-              tma_load_2d_pair(a, &p.g_mn[span.shift], m0, span.prev_g_row0 + k, bar);
-              tma_load_2d_pair(a + 8192, &p.g_mn[span.shift], m0 + 64, span.prev_g_row0 + k, bar);
+              tma_load_2d_pair(a, &p.g_mn[work.shift], m0, work.prev_g_row0 + k, bar);
+              tma_load_2d_pair(a + 8192, &p.g_mn[work.shift], m0 + 64, work.prev_g_row0 + k, bar);
             }
             tma_load_2d_pair(b, &p.x_mn[gathered], n0, k, bar);
             if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, k, bar);
@@ -444,7 +428,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
       for (bool first = true; ok; first = false) {
-        if (GRAD ? !next_announced() : !next_static(first)) break;
+        if (GRAD ? !next_announced(first) : !next_static(first)) break;
         if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) break;
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kTile);
@@ -478,18 +462,22 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
     int acc = 0;
     uint32_t acc_phase = 0;
     for (bool first = true;; first = false) {
-      if (GRAD ? !next_announced() : !next_static(first)) break;
+      if (GRAD ? !next_announced(first) : !next_static(first)) break;
       const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32;   // of this warp
       const int row = m0 + lane;
       const bool row_counts = row < rows;
       int label = -1;
-      float minus_lse2 = 0.f, weight = 0.f;
+      float shift2 = 0.f, weight = 0.f;
       if (t.kind == 0 && row_counts) {
         label = p.labels[row];
         if (GRAD) {
-          minus_lse2 = -p.row_lse[row] * kLog2e;
+          shift2 = p.row_shift[row];
           weight = p.row_weight[row];
         }
+      }
+      if (t.kind == 0 && p.bias != nullptr && lane < 4) {   // the tile's bias, a line per 64 columns, on its way while the tile is computed
+        const int col = work.col0 + t.n * p.block_n + lane * 64;
+        if (col < p.vocab) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.bias + col));
       }
       if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * acc, acc_phase, abort_flag))) break;
       tc_fence_after();
@@ -501,13 +489,15 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
         for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
           const int col = n0 + c;
           if (col >= p.vocab || m0 >= rows) break;
+          Bias32 bias;
+          load_bias(p.bias, col, p.vocab, bias);
           uint32_t v[32];
           tmem_ld_32x32(taddr0 + c, v);
           tmem_ld_wait();
           float z[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
-          add_bias(p.bias, col, p.vocab, z);
+          add_bias(p.bias, bias, z);
           if (col + 32 > p.vocab) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) if (col + j >= p.vocab) z[j] = -INFINITY;
@@ -534,34 +524,41 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
       } else if (t.kind == 0) {
         const int n0 = t.n * p.block_n;                 // in the piece
         const bool whole = __all_sync(0xffffffffu, row_counts);
-        bf16* g_out = p.g + static_cast<int64_t>(span.g_row0 + m0 + (lane & ~3)) * span.g_pitch + (lane & 3) * 8;
+        bf16* g_out = p.g + static_cast<int64_t>(work.g_row0 + m0 + (lane & ~3)) * g_pitch + (lane & 3) * 8;
 #pragma unroll 1
         for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
           const int local = n0 + c;
           // (in whole k-blocks of the products that sum over columns and over rows)
-          if (local >= (span.cols + 63) / 64 * 64 || m0 >= (rows + 63) / 64 * 64) break;
-          const int col = span.col0 + local;
+          if (local >= (work.cols + 63) / 64 * 64 || m0 >= (rows + 63) / 64 * 64) break;
+          const int col = work.col0 + local;
+          Bias32 bias;
+          load_bias(p.bias, col, p.vocab, bias);
           uint32_t v[32];
           tmem_ld_32x32(taddr0 + c, v);
           tmem_ld_wait();
           float g[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(v[j]);
-          add_bias(p.bias, col, p.vocab, g);
+          add_bias(p.bias, bias, g);
+          // |weight| exp(z - lse): the weight is in the exponent
 #pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, minus_lse2));
+          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, shift2));
+          if (__any_sync(0xffffffffu, weight < 0.f)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = weight < 0.f ? -g[j] : g[j];
+          }
           const int at = label - col;
           const bool hit = __any_sync(0xffffffffu, at >= 0 && at < 32);
           if (hit) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) if (j == at) g[j] -= 1.f;
-          }
-#pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] *= weight;
-          if (hit) {                                    // what rounding takes from the label's entry
             float mine = 0.f;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) if (j == at) mine = g[j];
+            for (int j = 0; j < 32; ++j) {
+              if (j == at) {
+                g[j] -= weight;
+                mine = g[j];
+              }
+            }
+            // what rounding takes from the label's entry
             if (at >= 0 && at < 32) p.row_residual[row] = mine - __bfloat162float(__float2bfloat16_rn(mine));
           }
           if (!whole) {                                 // (behind the last row lies anything)
@@ -579,15 +576,15 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
                                 pack_bf16(g[q * 8 + 6], g[q * 8 + 7]));
           exchange_pieces(out, lane);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(q) * span.g_pitch + local) = out[q];
+          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(q) * g_pitch + local) = out[q];
           if (p.bias_parts != nullptr && m0 < rows) {
             const float s = column_sums(g, lane);
-            if (local + lane < span.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + col + lane] = s;
+            if (local + lane < work.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + col + lane] = s;
           }
         }
       } else if (t.kind == 1) {
         const int n0 = t.n * p.block_h;
-        float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * span.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
+        float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * work.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
 #pragma unroll 1
         for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
           if (n0 + c >= p.hidden || m0 >= rows) break;
@@ -611,18 +608,18 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               float* to = sums + static_cast<int64_t>(q) * p.hidden + col;
-              if (span.prev_col0 == 0) *reinterpret_cast<uint4*>(to) = out[q]; else red_add_v4(to, out[q]);
+              if (work.prev_col0 == 0) *reinterpret_cast<uint4*>(to) = out[q]; else red_add_v4(to, out[q]);
             }
           }
         }
       } else {
         const int n0 = t.n * p.block_h;
-        const int word = span.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
+        const int word = work.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
         bf16* dw = p.dw + static_cast<int64_t>(word) * p.dw_stride + (lane & 3) * 8;
 #pragma unroll 1
         for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
           const int col = n0 + c;
-          if (col >= p.hidden || span.prev_col0 + m0 >= p.vocab) break;
+          if (col >= p.hidden || work.prev_col0 + m0 >= p.vocab) break;
           uint32_t v[32];
           if (t.k_blocks > 0) {
             tmem_ld_32x32(taddr0 + c, v);
@@ -632,7 +629,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
             for (int j = 0; j < 32; ++j) v[j] = 0u;
           }
           if (p.accumulate) {
-            const int mine = span.prev_col0 + row;
+            const int mine = work.prev_col0 + row;
             const bf16* old = p.dw + static_cast<int64_t>(mine) * p.dw_stride + col;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {               // (hidden is a multiple of eight)
@@ -680,6 +677,9 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
   }
 }
 
+// A row's part of the exponent of weight exp(z - lse), in powers of two (the sign of the weight is put in afterwards), and its weight.
+__device__ __forceinline__ float2 weighted_shift(float lse, float weight) { return make_float2(log2f(fabsf(weight)) - lse * kLog2e, weight); }
+
 // ---- few rows ------------------------------------------------------------------------------------
 
 // Up to 128 rows the products are taken turned: 128 words are the rows (lanes) of an accumulator and the rows of x, rounded up to sixteen,
@@ -692,7 +692,8 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
 //             the MN-major one for dx; db is a thread's own sum.  The hidden states are copied once with zeros in the rows without a label,
 //             for the product that sums over rows.
 constexpr int kFewRows = 128;
-constexpr int kFewThreads = 6 * 32;
+constexpr int kFewWarps = 8;             // of the epilogue: two per quarter of the words, which share the blocks of 32 rows
+constexpr int kFewThreads = (2 + kFewWarps) * 32;
 constexpr int kFewMaxStages = 12;
 constexpr int kFewStageA = 128 * 128;
 constexpr int kFewBook = 8192;
@@ -730,12 +731,14 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
   const uint32_t bar_empty = bar_full + 8 * kFewMaxStages;
   const uint32_t bar_acc_full = bar_empty + 8 * kFewMaxStages;
   const uint32_t bar_acc_empty = bar_acc_full + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * kFewMaxStages + 4));
+  const uint32_t bar_db = bar_acc_empty + 16;           // (backward) [accumulator][quarter]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * kFewMaxStages + 4 + 8));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* s_label = reinterpret_cast<int*>(book + 256);                    // of every row; -1 where it takes no part
-  float2* s_row = reinterpret_cast<float2*>(book + 256 + 512);          // (backward) -lse log2 e, weight
-  float2* s_part = reinterpret_cast<float2*>(book + 256 + 512 + 1024);  // (forward) [quarter][row]
-  static_assert(256 + 512 + 1024 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
+  int* s_label = reinterpret_cast<int*>(book + 512);                    // of every row; -1 where it takes no part
+  float2* s_row = reinterpret_cast<float2*>(book + 512 + 512);          // (backward) weighted_shift
+  float2* s_part = reinterpret_cast<float2*>(book + 512 + 512 + 1024);  // (forward) [quarter][row]
+  float* s_db = reinterpret_cast<float*>(s_part);                       // (backward) [accumulator][quarter][word]
+  static_assert(8 * (2 * kFewMaxStages + 12) + 8 <= 512 && 512 + 512 + 1024 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int stages = p.stages, stage_bytes = p.stage_bytes;
@@ -748,8 +751,9 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(bar_acc_full + 8 * a, 1);
-      mbar_init(bar_acc_empty + 8 * a, 4);
+      mbar_init(bar_acc_empty + 8 * a, kFewWarps);
     }
+    for (int i = 0; i < 8; ++i) mbar_init(bar_db + 8 * i, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -821,29 +825,32 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
   } else {
     // ------------------------------ epilogue ----------------------------------
     const int quarter = warp & 3;
-    const int row0 = tid - 64;                                      // the row that this thread fetches the label of
-    int label = row0 < p.rows ? p.labels[row0] : -1;
-    if (GRAD && label >= p.vocab && blockIdx.x == 0 && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
-    if (label >= p.vocab) label = -1;
-    s_label[row0] = label;
-    if (GRAD)
-      s_row[row0] = label >= 0 ? make_float2(-p.lse[row0] * kLog2e, p.grad_loss != nullptr ? p.grad_loss[row0] : 1.f) : make_float2(0.f, 0.f);
-    asm volatile("bar.sync 1, 128;" ::: "memory");                 // (the epilogue warps; nothing that can give up comes before it)
+    const int half = (warp - 2) >> 2;                               // of the two warps of the quarter
+    const int first = tid - 64;
+    if (first < kFewRows) {
+      int label = first < p.rows ? p.labels[first] : -1;
+      if (GRAD && label >= p.vocab && blockIdx.x == 0 && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
+      if (label >= p.vocab) label = -1;
+      s_label[first] = label;
+      if (GRAD)
+        s_row[first] = label >= 0 ? weighted_shift(p.lse[first], p.grad_loss != nullptr ? p.grad_loss[first] : 1.f) : make_float2(0.f, 0.f);
+    }
+    // (the epilogue warps; nothing that can give up comes before it)
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kFewWarps) : "memory");
     if (GRAD && p.x_clean != nullptr) {
       // (rows of hidden states, those without a part as zeros, in whole k-blocks of the product over rows)
       const int vectors = p.hidden / 8;
       for (int r = blockIdx.x; r < p.g_pitch; r += gridDim.x) {
         const bool there = s_label[r] >= 0;
-        for (int c = row0; c < vectors; c += 128)
+        for (int c = first; c < vectors; c += 32 * kFewWarps)
           reinterpret_cast<uint4*>(p.x_clean + static_cast<int64_t>(r) * p.hidden)[c] =
               there ? __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(r) * p.x_stride) + c) : make_uint4(0, 0, 0, 0);
       }
     }
-    if (GRAD && blockIdx.x == 0 && row0 == 0) *p.counter = 0;
+    if (GRAD && blockIdx.x == 0 && first == 0) *p.counter = 0;
     float2* my_part = s_part + quarter * kFewRows + lane;           // (forward) largest logit and sum of row 32 * i + lane
     if (!GRAD) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) my_part[i * 32] = make_float2(kFloor, 0.f);
+      for (int i = half; i < 4; i += 2) my_part[i * 32] = make_float2(kFloor, 0.f);
     }
     int acc = 0;
     uint32_t acc_phase = 0;
@@ -858,7 +865,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
       const int chunks = ((GRAD ? p.g_pitch : p.rows) + 31) / 32;
       // (not unrolled: four copies of the body are more than the instruction cache holds; the first tile took 13 k clocks with them)
 #pragma unroll 1
-      for (int i = 0; i < chunks; ++i) {
+      for (int i = half; i < chunks; i += 2) {
         uint32_t v[32];
         tmem_ld_32x32(taddr0 + i * 32, v);
         tmem_ld_wait();
@@ -890,18 +897,22 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
           const uint32_t counts = __ballot_sync(0xffffffffu, my_label >= 0);
 #pragma unroll
           for (int j = 0; j < 32; ++j) z[j] = ex2_approx(fmaf(z[j], kLog2e, s_row[i * 32 + j].x));
+          const uint32_t negative = __ballot_sync(0xffffffffu, s_row[i * 32 + lane].y < 0.f);
+          if (negative != 0) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z[j] = ((negative >> j) & 1u) ? -z[j] : z[j];
+          }
           if (hits != 0) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
               if (((hits >> j) & 1u) && s_label[i * 32 + j] == word) {
-                z[j] -= 1.f;
-                const float entry = z[j] * s_row[i * 32 + j].y;      // what rounding takes from the label's entry
-                p.row_residual[i * 32 + j] = entry - __bfloat162float(__float2bfloat16_rn(entry));
+                z[j] -= s_row[i * 32 + j].y;
+                p.row_residual[i * 32 + j] = z[j] - __bfloat162float(__float2bfloat16_rn(z[j]));   // what rounding takes from the label's entry
               }
             }
           }
 #pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = ((counts >> j) & 1u) && is_word ? z[j] * s_row[i * 32 + j].y : 0.f;
+          for (int j = 0; j < 32; ++j) z[j] = ((counts >> j) & 1u) && is_word ? z[j] : 0.f;
           float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < 32; ++j) s[j & 3] += z[j];
@@ -917,7 +928,19 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
           for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g + q * p.g_pitch) = out[q];
         }
       }
-      if (GRAD && p.db != nullptr && is_word) p.db[word] = p.accumulate ? p.db[word] + db : db;
+      if (GRAD && p.db != nullptr && chunks > 1) {                 // the sums of the other warp's rows
+        float* other = s_db + (acc * 4 + quarter) * 32 + lane;
+        const uint32_t bar = bar_db + 8 * (acc * 4 + quarter);
+        if (half == 1) {
+          *other = db;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar);
+        } else {
+          if (!__all_sync(0xffffffffu, mbar_wait(bar, acc_phase, abort_flag))) break;
+          db += *other;
+        }
+      }
+      if (GRAD && p.db != nullptr && half == 0 && is_word) p.db[word] = p.accumulate ? p.db[word] + db : db;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_acc_empty + 8 * acc);
@@ -959,17 +982,31 @@ __host__ __device__ inline int choose_ranges(int rows, int piece, int pieces, in
   return ranges < kMaxRanges ? static_cast<int>(ranges) : kMaxRanges;
 }
 
-// The cut for `rows` rows: pieces as wide as the buffers hold for so many, as few ranges as keep the pairs busy.
-__device__ inline void make_plan(const VocabRowsParams& p, int rows) {
-  VocabPlan plan;
-  plan.rows = rows;
-  plan.row_pitch = max(1, (rows + kTile - 1) / kTile) * kTile;
-  plan.shift = 0;
-  while (plan.shift < p.max_shift && (p.buffer_rows >> (plan.shift + 1)) >= plan.row_pitch) ++plan.shift;
-  plan.piece = p.piece << plan.shift;
-  plan.pieces = (p.vocab + plan.piece - 1) / plan.piece;
-  plan.ranges = min(choose_ranges(rows, min(plan.piece, p.vocab), plan.pieces, p.hidden, p.block_h), p.dx_rows / plan.row_pitch);
-  *p.plan = plan;
+// The cut for `rows` rows: pieces as wide as the buffers hold for so many, as few ranges as keep the pairs busy.  One thread per launch.
+__device__ inline void make_work(const VocabRowsParams& p, int rows, int index) {
+  VocabWork w = {};
+  w.rows = rows;
+  w.row_tiles = (rows + kTile - 1) / kTile;
+  w.row_pitch = max(1, w.row_tiles) * kTile;
+  while (w.shift < p.max_shift && (p.buffer_rows >> (w.shift + 1)) >= w.row_pitch) ++w.shift;
+  const int piece = p.piece << w.shift, pieces = (p.vocab + piece - 1) / piece, hidden_tiles = (p.hidden + p.block_h - 1) / p.block_h;
+  w.ranges = min(choose_ranges(rows, min(piece, p.vocab), pieces, p.hidden, p.block_h), p.dx_rows / w.row_pitch);
+  if (index < pieces) {
+    w.col0 = index * piece;
+    w.cols = min(piece, p.vocab - w.col0);
+    w.g_row0 = (index & (p.buffers - 1)) * (p.buffer_rows >> w.shift);
+    w.n0 = w.row_tiles * ((w.cols + kTile - 1) / kTile);
+  }
+  if (index > 0 && index <= pieces) {
+    w.prev_col0 = (index - 1) * piece;
+    w.prev_cols = min(piece, p.vocab - w.prev_col0);
+    w.prev_g_row0 = ((index - 1) & (p.buffers - 1)) * (p.buffer_rows >> w.shift);
+    w.n1 = p.want_x ? w.row_tiles * hidden_tiles * w.ranges : 0;
+    w.n2 = p.want_w ? (w.prev_cols + kTile - 1) / kTile * hidden_tiles : 0;
+    w.k1 = ((w.prev_cols + 63) / 64 + w.ranges - 1) / w.ranges;
+    w.k2 = (rows + 63) / 64;
+  }
+  p.work[index] = w;
 }
 
 // A CTA per `rows_per_cta` rows counts the labels before them and all of them (a few KB that stay in L2), and gives every row with a
@@ -1006,11 +1043,11 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
   __syncthreads();
   all = s_all;
   if (blockIdx.x == 0) {
-    if (tid == 0) {
-      *p.count = all;
-      if (p.plan != nullptr) make_plan(p, all);
+    if (tid == 0) *p.count = all;
+    for (int i = tid; i < p.n_counters; i += kRowsThreads) {
+      p.counters[i] = 0;
+      make_work(p, all, i);
     }
-    for (int i = tid; i < p.n_counters; i += kRowsThreads) p.counters[i] = 0;
   }
   const int vectors = p.hidden / 8;
   for (int r0 = first; r0 < last; r0 += kRowsThreads) {
@@ -1029,8 +1066,11 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
       if (has) {
         p.row_of[place] = r;
         p.row_label[place] = p.labels[r];
-        if (p.row_lse != nullptr) p.row_lse[place] = p.lse[r];
-        if (p.row_weight != nullptr) p.row_weight[place] = p.grad_loss != nullptr ? p.grad_loss[r] : 1.f;
+        if (p.row_shift != nullptr) {
+          const float2 shift = weighted_shift(p.lse[r], p.grad_loss != nullptr ? p.grad_loss[r] : 1.f);
+          p.row_shift[place] = shift.x;
+          p.row_weight[place] = shift.y;
+        }
       } else if (p.loss_out != nullptr) {
         p.loss_out[r] = 0.f;
         p.lse_out[r] = 0.f;
@@ -1063,6 +1103,7 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
 // ---- a row's tiles put together ------------------------------------------------------------------
 
 constexpr int kJoinThreads = 128;
+constexpr int kSharedUnits = 1024;
 
 // A warp per row: log-sum-exp and loss from (largest logit, sum) of every half tile.
 __global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __grid_constant__ VocabJoinParams p) {
@@ -1102,64 +1143,91 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __g
   }
 }
 
+// The last launch of a gradient.
 // dx: the ranges of a row added up in order, and what rounding took from the label's entry of g times the label's row of W (that one entry
 // is most of a row of g: without this a row of dx would be off by its rounding); rounded once, to the row's place; zeros for rows without
 // a label.  A warp per row and 256 columns.
-__global__ void __launch_bounds__(kJoinThreads) vocab_dx_kernel(const __grid_constant__ VocabDxParams p) {
+// db (the first db_ctas CTAs): the sums of all blocks of 32 rows, in order; a CTA per 32 columns, every warp each fourth block.
+__global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid_constant__ VocabFinishParams p) {
+  __shared__ float s_sum[kJoinThreads / 32][32];
+  __shared__ float s_acc[kJoinThreads / 32][8][32];
   grid_dependency_wait();
   grid_launch_dependents();
-  const int lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (static_cast<int>(blockIdx.x) < p.db_ctas) {
+    const int blocks = (__ldcg(&p.work->rows) + 31) / 32;
+    const int col = blockIdx.x * 32 + lane;
+    float sum = 0.f;
+    if (col < p.vocab) {
+#pragma unroll 8
+      for (int b = warp; b < blocks; b += kJoinThreads / 32) sum += p.bias_parts[static_cast<int64_t>(b) * p.vocab + col];
+    }
+    s_sum[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0 || col >= p.vocab) return;
+    for (int w = 1; w < kJoinThreads / 32; ++w) sum += s_sum[w][lane];
+    p.db[col] = p.accumulate ? p.db[col] + sum : sum;
+    return;
+  }
   const int blocks = (p.hidden + 255) / 256;
-  const int ranges = p.plan != nullptr ? p.plan->ranges : p.ranges;
-  const int64_t row_pitch = p.plan != nullptr ? p.plan->row_pitch : p.row_pitch;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * (kJoinThreads / 32), units = static_cast<int64_t>(p.rows) * blocks;
-  for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); u < units; u += step) {
+  const int ranges = p.work != nullptr ? __ldcg(&p.work->ranges) : p.ranges;
+  const int64_t row_pitch = p.work != nullptr ? __ldcg(&p.work->row_pitch) : p.row_pitch;
+  // With many ranges the four warps of a CTA share a unit, every fourth range each, if there are so few units that all of them run at
+  // once (77 rows x 768 in 18 ranges 7.6 -> 5.1 us; 4096 x 768, 614 of them in 9 ranges, 11 -> 17).
+  const int64_t units = static_cast<int64_t>(p.rows) * blocks;
+  const bool shared = ranges >= 2 * kJoinThreads / 32 && units <= kSharedUnits;
+  const int share = shared ? kJoinThreads / 32 : 1;
+  const int64_t step = static_cast<int64_t>(gridDim.x - p.db_ctas) * (shared ? 1 : kJoinThreads / 32);
+  const int64_t cta = blockIdx.x - p.db_ctas;
+  for (int64_t u = shared ? cta : cta * (kJoinThreads / 32) + warp; u < units; u += step) {
     const int row = static_cast<int>(u / blocks), c = static_cast<int>(u % blocks) * 256 + lane * 8;
-    if (c >= p.hidden) continue;
+    const bool inside = c < p.hidden;
     const int label = p.labels[row];
-    const bool counts = label >= 0 && label < p.vocab;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-    if (counts) {
-      const int place = p.place_of != nullptr ? p.place_of[row] : row;
+    const int place = p.place_of != nullptr ? p.place_of[row] : row;
+    bf16* out = p.dx + static_cast<int64_t>(row) * p.dx_stride + c;
+    if (label < 0 || label >= p.vocab) {                  // (the same for all who share a unit)
+      if (inside && (!shared || warp == 0)) *reinterpret_cast<uint4*>(out) = make_uint4(0, 0, 0, 0);
+      continue;
+    }
+    float acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    if (inside) {
       const float* src = p.sums + static_cast<int64_t>(place) * p.hidden + c;
       const uint4 word = __ldg(reinterpret_cast<const uint4*>(p.w + static_cast<int64_t>(label) * p.w_stride + c));
       const float residual = p.row_residual[place];
-#pragma unroll 8
-      for (int s = 0; s < ranges; ++s) {
+#pragma unroll 4
+      for (int s = shared ? warp : 0; s < ranges; s += share) {
         const float4* f = reinterpret_cast<const float4*>(src + s * row_pitch * p.hidden);
-        const float4 x = f[0], w = f[1];
-        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-        b.x += w.x; b.y += w.y; b.z += w.z; b.w += w.w;
+        const float4 x = f[0], y = f[1];
+        acc[0] += x.x; acc[1] += x.y; acc[2] += x.z; acc[3] += x.w;
+        acc[4] += y.x; acc[5] += y.y; acc[6] += y.z; acc[7] += y.w;
       }
-      a.x = fmaf(residual, bf16_lo(word.x), a.x); a.y = fmaf(residual, bf16_hi(word.x), a.y);
-      a.z = fmaf(residual, bf16_lo(word.y), a.z); a.w = fmaf(residual, bf16_hi(word.y), a.w);
-      b.x = fmaf(residual, bf16_lo(word.z), b.x); b.y = fmaf(residual, bf16_hi(word.z), b.y);
-      b.z = fmaf(residual, bf16_lo(word.w), b.z); b.w = fmaf(residual, bf16_hi(word.w), b.w);
+      if (!shared || warp == 0) {
+        const uint32_t w[4] = {word.x, word.y, word.z, word.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          acc[2 * j] = fmaf(residual, bf16_lo(w[j]), acc[2 * j]);
+          acc[2 * j + 1] = fmaf(residual, bf16_hi(w[j]), acc[2 * j + 1]);
+        }
+      }
     }
-    *reinterpret_cast<uint4*>(p.dx + static_cast<int64_t>(row) * p.dx_stride + c) =
-        make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+    if (shared) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s_acc[warp][j][lane] = acc[j];
+      __syncthreads();
+      if (warp == 0) {
+        for (int w = 1; w < kJoinThreads / 32; ++w) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[j] += s_acc[w][j][lane];
+        }
+      }
+      __syncthreads();
+      if (warp != 0) continue;
+    }
+    if (inside)
+      *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
   }
-}
-
-// db: the sums of all blocks of 32 rows, in order.  A CTA per 32 columns; every warp takes each eighth block.
-__global__ void __launch_bounds__(256) vocab_bias_kernel(const __grid_constant__ VocabBiasParams p) {
-  __shared__ float s_sum[8][32];
-  grid_dependency_wait();
-  grid_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rows = min(p.rows, *reinterpret_cast<const volatile int*>(p.count));
-  const int blocks = (rows + 31) / 32;
-  const int col = blockIdx.x * 32 + lane;
-  float sum = 0.f;
-  if (col < p.cols) {
-#pragma unroll 8
-    for (int b = warp; b < blocks; b += 8) sum += p.parts[static_cast<int64_t>(b) * p.pitch + col];
-  }
-  s_sum[warp][lane] = sum;
-  __syncthreads();
-  if (warp != 0 || col >= p.cols) return;
-  for (int w = 1; w < 8; ++w) sum += s_sum[w][lane];
-  p.out[col] = p.accumulate ? p.out[col] + sum : sum;
 }
 
 template <bool GRAD>
@@ -1242,7 +1310,7 @@ struct GradPlan {
   int piece, pieces, buffers, block_h, ranges, g_pitch, max_shift;
   bool few;
   int64_t row_pitch, dx_rows;
-  size_t count, plan, counters, row_of, row_label, row_lse, row_weight, row_residual, place_of, gathered, g, dx, bias_parts, bytes;
+  size_t count, work, counters, row_of, row_label, row_shift, row_weight, row_residual, place_of, gathered, g, dx, bias_parts, bytes;
 };
 GradPlan grad_plan(int rows, int vocab, int hidden) {
   GradPlan f;
@@ -1266,11 +1334,11 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += whole_lines(bytes); return here; };
   f.count = take(256);
-  f.plan = take(sizeof(VocabPlan));
+  f.work = take((static_cast<size_t>(f.pieces) + 1) * sizeof(VocabWork));
   f.counters = take((static_cast<size_t>(f.pieces) + 1) * 4);
   f.row_of = take(f.row_pitch * 4);
   f.row_label = take(f.row_pitch * 4);
-  f.row_lse = take(f.row_pitch * 4);
+  f.row_shift = take(f.row_pitch * 4);
   f.row_weight = take(f.row_pitch * 4);
   f.row_residual = take(f.row_pitch * 4);
   f.place_of = take(f.row_pitch * 4);
@@ -1283,8 +1351,8 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
 }
 
 void launch_rows_setup(VocabRowsParams* r, int* ctas) {
-  // at most 1024 CTAs, each of which reads all labels
-  r->rows_per_cta = ceil_div(r->rows, 1024) > 32 ? ceil_div(r->rows, 1024) : 32;
+  // a row per warp and CTA (the copies of a warp come one after the other), but at most 1024 CTAs, each of which reads all labels
+  r->rows_per_cta = ceil_div(r->rows, 1024) > 8 ? ceil_div(r->rows, 1024) : 8;
   *ctas = ceil_div(r->rows, r->rows_per_cta);
 }
 template <typename T>
@@ -1329,6 +1397,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
   p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
   p.labels = f.gather ? at<int32_t>(ws, f.row_label) : c.labels;
   p.count = f.gather ? at<int32_t>(ws, f.count) : nullptr;
+  p.n_tiles = f.tiles_n;
   p.label_logit = at<float>(ws, f.label_logit); p.parts = at<float2>(ws, f.parts); p.part_pitch = f.part_pitch; p.status = c.status;
   if ((e = encode_matrix_map(&p.x_k[0], c.x, c.rows, c.hidden, c.x_stride * 2, kHalf, 64, false)) != cudaSuccess) return e;
   p.x_k[1] = p.x_k[0];
@@ -1350,22 +1419,27 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   const GradPlan f = grad_plan(c.rows, c.vocab, c.hidden);
   void* ws = c.workspace;
   cudaError_t e;
-  VocabDxParams d;
+  VocabFinishParams d;
   memset(&d, 0, sizeof(d));
   d.sums = at<float>(ws, f.dx); d.labels = c.labels; d.row_residual = at<float>(ws, f.row_residual); d.w = c.w; d.w_stride = c.w_stride;
   d.dx = c.dx; d.dx_stride = c.dx_stride; d.rows = c.rows; d.vocab = c.vocab; d.hidden = c.hidden; d.row_pitch = f.row_pitch; d.ranges = f.ranges;
-  const int64_t dx_units = (static_cast<int64_t>(c.rows) * ceil_div(c.hidden, 256) + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
-  const dim3 dx_ctas(static_cast<unsigned>(dx_units < 16 * sm_count ? dx_units : 16 * sm_count));
+  d.db = c.db; d.accumulate = c.accumulate;
+  unsigned dx_ctas = 0;
+  if (c.dx != nullptr) {
+    // a CTA per unit where its warps may share one, otherwise a warp
+    const int64_t units = static_cast<int64_t>(c.rows) * ceil_div(c.hidden, 256);
+    const int64_t ctas = units <= kSharedUnits ? units : (units + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
+    dx_ctas = static_cast<unsigned>(ctas < 64 * sm_count ? ctas : 64 * sm_count);
+  }
   bf16* gathered = at<bf16>(ws, f.gathered);
   bf16* g = at<bf16>(ws, f.g);
   const int64_t h_stride = static_cast<int64_t>(c.hidden) * 2;
   const bool products = c.dx != nullptr || c.dw != nullptr;
-  const int row_tiles = static_cast<int>(f.row_pitch / kTile), hidden_tiles = ceil_div(c.hidden, f.block_h);
   VocabLossParams p;
   memset(&p, 0, sizeof(p));
   p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias; p.status = c.status;
   p.dx_sums = at<float>(ws, f.dx);
-  p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate;
+  p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate; p.n_tiles = ceil_div(c.hidden, f.block_h);
   p.dw = c.dw; p.dw_stride = c.dw_stride;
   if ((e = encode_matrix_map(&p.w_mn, c.w, c.vocab, c.hidden, c.w_stride * 2, 64, 64, false)) != cudaSuccess) return e;
 
@@ -1389,27 +1463,28 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     p.x_mn[1] = p.x_mn[0];
     p.x_k[0] = p.w_k = p.w_mn;      // (of kind 0, which has no tiles here)
     p.by_words = 1; p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.counter = w.counter;
-    const int tiles = row_tiles * hidden_tiles * f.ranges + ceil_div(c.vocab, kTile) * hidden_tiles;
+    p.range_blocks = ceil_div(ceil_div(c.vocab, 64), f.ranges);
+    const int tiles = p.n_tiles * (f.ranges + ceil_div(c.vocab, kTile));
     if ((e = launch_pairs<true>(p, tiles, sm_count, stream)) != cudaSuccess || c.dx == nullptr) return e;
-    return launch_kernel(vocab_dx_kernel, dx_ctas, dim3(kJoinThreads), 0, stream, d);
+    return launch_kernel(vocab_finish_kernel, dim3(dx_ctas), dim3(kJoinThreads), 0, stream, d);
   }
 
   VocabRowsParams r;
   memset(&r, 0, sizeof(r));
   r.labels = c.labels; r.x = c.x; r.x_stride = c.x_stride; r.rows = c.rows; r.vocab = c.vocab; r.hidden = c.hidden;
   r.count = at<int32_t>(ws, f.count); r.row_of = at<int32_t>(ws, f.row_of); r.row_label = at<int32_t>(ws, f.row_label);
-  r.row_lse = at<float>(ws, f.row_lse); r.row_weight = at<float>(ws, f.row_weight); r.place_of = at<int32_t>(ws, f.place_of);
+  r.row_shift = at<float>(ws, f.row_shift); r.row_weight = at<float>(ws, f.row_weight); r.place_of = at<int32_t>(ws, f.place_of);
   r.lse = c.lse; r.grad_loss = c.grad_loss; r.gathered = at<bf16>(ws, f.gathered);
   r.counters = at<uint32_t>(ws, f.counters); r.n_counters = f.pieces + 1; r.status = c.status;
-  r.plan = at<VocabPlan>(ws, f.plan); r.piece = f.piece; r.max_shift = f.max_shift; r.buffer_rows = static_cast<int>(f.row_pitch);
-  r.dx_rows = static_cast<int>(f.dx_rows); r.block_h = f.block_h;
+  r.work = at<VocabWork>(ws, f.work); r.piece = f.piece; r.max_shift = f.max_shift; r.buffers = f.buffers; r.buffer_rows = static_cast<int>(f.row_pitch);
+  r.dx_rows = static_cast<int>(f.dx_rows); r.block_h = f.block_h; r.want_x = c.dx != nullptr ? 1 : 0; r.want_w = c.dw != nullptr ? 1 : 0;
   int ctas = 0;
   launch_rows_setup(&r, &ctas);
   if ((e = launch_kernel(vocab_rows_kernel, dim3(ctas), dim3(kRowsThreads), 0, stream, r)) != cudaSuccess) return e;
 
-  p.labels = r.row_label; p.plan = r.plan; p.row_lse = r.row_lse; p.row_weight = r.row_weight; p.row_residual = at<float>(ws, f.row_residual);
+  p.labels = r.row_label; p.row_shift = r.row_shift; p.row_weight = r.row_weight; p.row_residual = at<float>(ws, f.row_residual);
   p.bias_parts = c.db != nullptr ? at<float>(ws, f.bias_parts) : nullptr; p.bias_pitch = c.vocab;
-  p.g = g; p.buffers = f.buffers; p.buffer_rows = static_cast<int>(f.row_pitch);
+  p.g = g; p.piece = f.piece;
   if ((e = encode_matrix_map(&p.x_k[0], c.x, c.rows, c.hidden, c.x_stride * 2, kHalf, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_k[1], gathered, f.row_pitch, c.hidden, h_stride, kHalf, 64, false)) != cudaSuccess ||
       (e = encode_matrix_map(&p.x_mn[0], c.x, c.rows, c.hidden, c.x_stride * 2, 64, 64, false)) != cudaSuccess ||
@@ -1424,19 +1499,13 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   }
   // (sized for all rows; with fewer, the pieces are wider and the last launches find nothing to do)
   for (int j = 0; j <= f.pieces && (j < f.pieces || products); ++j) {
-    p.index = j;
+    p.work = r.work + j;
     p.counter = r.counters + j;
     if ((e = launch_pairs<true>(p, sm_count, sm_count, stream)) != cudaSuccess) return e;
   }
-  if (c.db != nullptr) {
-    VocabBiasParams b;
-    memset(&b, 0, sizeof(b));
-    b.parts = p.bias_parts; b.pitch = c.vocab; b.count = r.count; b.rows = c.rows; b.cols = c.vocab; b.out = c.db; b.accumulate = c.accumulate;
-    if ((e = launch_kernel(vocab_bias_kernel, dim3(ceil_div(c.vocab, 32)), dim3(256), 0, stream, b)) != cudaSuccess) return e;
-  }
-  if (c.dx == nullptr) return cudaSuccess;
-  d.place_of = r.place_of; d.plan = r.plan;
-  return launch_kernel(vocab_dx_kernel, dx_ctas, dim3(kJoinThreads), 0, stream, d);
+  if (c.dx == nullptr && c.db == nullptr) return cudaSuccess;
+  d.place_of = r.place_of; d.work = r.work; d.bias_parts = p.bias_parts; d.db_ctas = c.db != nullptr ? ceil_div(c.vocab, 32) : 0;
+  return launch_kernel(vocab_finish_kernel, dim3(dx_ctas + d.db_ctas), dim3(kJoinThreads), 0, stream, d);
 }
 
 }  // namespace mt
