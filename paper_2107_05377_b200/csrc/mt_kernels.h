@@ -513,7 +513,8 @@ struct VocabLossParams {
   int32_t row_pitch, ranges, range_blocks;   // (few rows; k-blocks of a range)
   int32_t part_pitch, bias_pitch;
   int32_t want_x, want_w, accumulate;
-  int32_t by_words;            // g lies by words, [vocab][rows] (few rows; g_k: boxes of 128 words, g_mn: of 64)
+  int32_t by_words;            // g lies by words, [vocab][two terms][rows] (few rows; g_k: boxes of 128 words, g_mn: of 64)
+  const int32_t* two_terms;    // few rows: for every 256 words, whether the second term is there; or null
 };
 // Up to 128 rows: the logits turned, words on the lanes.
 struct VocabFewParams {
@@ -527,7 +528,8 @@ struct VocabFewParams {
   const bf16* x;
   int64_t x_stride;
   bf16* x_clean;               // [g_pitch][hidden], zeros in rows without a label; or null
-  bf16* g;                     // [vocab in whole tiles][g_pitch]
+  bf16* g;                     // [vocab in whole tiles][two terms][g_pitch]
+  int32_t* two_terms;          // for every 256 words: whether the second term is there
   float* db;
   float* row_residual;
   uint32_t* counter;           // set to zero (for the products)

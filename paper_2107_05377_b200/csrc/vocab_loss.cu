@@ -147,7 +147,7 @@ struct Tile {
 // The tiles of a launch in the order in which they are handed out, long ones first.  n_tiles: of the columns of a matrix product (forward:
 // the vocabulary; backward, kinds 1 and 2: the hidden size).
 template <bool GRAD>
-__device__ __forceinline__ Tile find_tile(const VocabWork& w, int n_tiles, int k0, int i) {
+__device__ __forceinline__ Tile find_tile(const VocabWork& w, int n_tiles, int k0, const int32_t* two_terms, int i) {
   Tile t;
   t.range = 0;
   t.k_begin = 0;
@@ -172,6 +172,8 @@ __device__ __forceinline__ Tile find_tile(const VocabWork& w, int n_tiles, int k
       t.n = divide(i, m_tiles, __frcp_rn(static_cast<float>(m_tiles)));
       t.m = i - t.n * m_tiles;
       t.k_blocks = w.k2;
+      // (few rows: g in two terms, one behind the other along K, where one of the words is a label)
+      if (two_terms != nullptr && i < w.n2 && __ldcg(two_terms + t.m) != 0) t.k_blocks = 2 * w.k2;
     }
     return t;
   }
@@ -309,7 +311,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
   // (Which pair computes a tile has no influence on it.)
   int slot = 0;
   uint32_t slot_phase = 0;
-  Tile t = find_tile<GRAD>(work, p.n_tiles, k0, worker);
+  Tile t = find_tile<GRAD>(work, p.n_tiles, k0, p.two_terms, worker);
   // Forward: m and n of the next tile of this worker without a division per tile.
   const int step_m = n_workers % max(work.row_tiles, 1), step_n = n_workers / max(work.row_tiles, 1);
   int at_tile = worker;
@@ -353,7 +355,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
     Tile ahead = t;
     if (worker >= total) ahead.kind = -1;
     auto announce = [&](int i) -> bool {
-      if (i < total) ahead = find_tile<GRAD>(work, p.n_tiles, k0, i); else ahead.kind = -1;
+      if (i < total) ahead = find_tile<GRAD>(work, p.n_tiles, k0, p.two_terms, i); else ahead.kind = -1;
       if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) return false;
       if (lane < 2)
         send_words(map_to_cta(smem_u32(const_cast<int4*>(slot_tile) + slot), lane), ahead.kind, ahead.m, ahead.n | (ahead.range << 16), ahead.k_blocks,
@@ -401,8 +403,9 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
               tma_load_2d_pair(a, &p.g_mn[work.shift], m0, work.prev_g_row0 + k, bar);
               tma_load_2d_pair(a + 8192, &p.g_mn[work.shift], m0 + 64, work.prev_g_row0 + k, bar);
             }
-            tma_load_2d_pair(b, &p.x_mn[gathered], n0, k, bar);
-            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, k, bar);
+            const int kx = p.by_words && kb >= work.k2 ? k - work.k2 * 64 : k;   // (both terms meet the same rows of x)
+            tma_load_2d_pair(b, &p.x_mn[gathered], n0, kx, bar);
+            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, kx, bar);
           }
         }
         ++issued;
@@ -689,7 +692,9 @@ __device__ __forceinline__ float2 weighted_shift(float lse, float weight) { retu
 //   forward   largest logit and sum of exponentials of a row over the 32 words of a warp: halves of the rows are exchanged for halves of the
 //             words (as column_sums), running over the CTA's tiles; the four warps are put together at the end
 //   backward  g by words, [vocab][64 or 128 rows], zeros in rows without a label and behind the last: as it is the operand along K for dW and
-//             the MN-major one for dx; db is a thread's own sum.  The hidden states are copied once with zeros in the rows without a label,
+//             the MN-major one for dx; db is a thread's own sum.  A row of dW whose word is a label is little else than that entry of g
+//             times a row of x, and with so few rows such entries are most of dW: where one of 256 words is a label, g of all of them is
+//             kept in two bf16 terms, which the product for dW takes one behind the other along K.  The hidden states are copied once with zeros in the rows without a label,
 //             for the product that sums over rows.
 constexpr int kFewRows = 128;
 constexpr int kFewWarps = 8;             // of the epilogue: two per quarter of the words, which share the blocks of 32 rows
@@ -862,6 +867,17 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
       tc_fence_after();
       const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc * kFewRows);
       float db = 0.f;
+      bool two_terms = false;                                       // one of the 256 words that a tile of dW has is a label
+      if (GRAD) {
+        bool mine = false;
+#pragma unroll
+        for (int i = 0; i < kFewRows / 32; ++i) {
+          const int l = s_label[i * 32 + lane];
+          mine |= l >= 0 && (l >> 8) == (tile >> 1);
+        }
+        two_terms = __any_sync(0xffffffffu, mine);
+        if ((tile & 1) == 0 && quarter == 0 && half == 0 && lane == 0) p.two_terms[tile >> 1] = two_terms ? 1 : 0;
+      }
       const int chunks = ((GRAD ? p.g_pitch : p.rows) + 31) / 32;
       // (not unrolled: four copies of the body are more than the instruction cache holds; the first tile took 13 k clocks with them)
 #pragma unroll 1
@@ -923,9 +939,20 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
             out[q] = make_uint4(pack_bf16(z[q * 8], z[q * 8 + 1]), pack_bf16(z[q * 8 + 2], z[q * 8 + 3]), pack_bf16(z[q * 8 + 4], z[q * 8 + 5]),
                                 pack_bf16(z[q * 8 + 6], z[q * 8 + 7]));
           exchange_pieces(out, lane);
-          bf16* g = p.g + static_cast<int64_t>(word0 + (lane & ~3)) * p.g_pitch + i * 32 + (lane & 3) * 8;
+          bf16* g = p.g + static_cast<int64_t>(word0 + (lane & ~3)) * (2 * p.g_pitch) + i * 32 + (lane & 3) * 8;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g + q * p.g_pitch) = out[q];
+          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g + q * 2 * p.g_pitch) = out[q];
+          if (two_terms) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z[j] -= __bfloat162float(__float2bfloat16_rn(z[j]));
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              out[q] = make_uint4(pack_bf16(z[q * 8], z[q * 8 + 1]), pack_bf16(z[q * 8 + 2], z[q * 8 + 3]), pack_bf16(z[q * 8 + 4], z[q * 8 + 5]),
+                                  pack_bf16(z[q * 8 + 6], z[q * 8 + 7]));
+            exchange_pieces(out, lane);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g + p.g_pitch + q * 2 * p.g_pitch) = out[q];
+          }
         }
       }
       if (GRAD && p.db != nullptr && chunks > 1) {                 // the sums of the other warp's rows
@@ -1310,7 +1337,7 @@ struct GradPlan {
   int piece, pieces, buffers, block_h, ranges, g_pitch, max_shift;
   bool few;
   int64_t row_pitch, dx_rows;
-  size_t count, work, counters, row_of, row_label, row_shift, row_weight, row_residual, place_of, gathered, g, dx, bias_parts, bytes;
+  size_t count, work, counters, row_of, row_label, row_shift, row_weight, row_residual, place_of, gathered, g, two_terms, dx, bias_parts, bytes;
 };
 GradPlan grad_plan(int rows, int vocab, int hidden) {
   GradPlan f;
@@ -1343,7 +1370,8 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.row_residual = take(f.row_pitch * 4);
   f.place_of = take(f.row_pitch * 4);
   f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
-  f.g = take(static_cast<size_t>(f.buffers) * (f.few ? f.g_pitch : f.row_pitch) * f.piece * 2);
+  f.g = take(static_cast<size_t>(f.buffers) * (f.few ? 2 * f.g_pitch : f.row_pitch) * f.piece * 2);
+  f.two_terms = take(f.few ? static_cast<size_t>(f.piece / kTile) * 4 : 0);
   f.dx = take(static_cast<size_t>(f.dx_rows) * hidden * 4);
   f.bias_parts = take(f.few ? 0 : static_cast<size_t>(f.row_pitch / 32) * vocab * 4);
   f.bytes = at;
@@ -1449,20 +1477,21 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
     w.lse = c.lse; w.grad_loss = c.grad_loss; w.x = c.x; w.x_stride = c.x_stride; w.x_clean = c.dw != nullptr ? gathered : nullptr;
     w.g = g; w.g_pitch = f.g_pitch; w.db = c.db; w.accumulate = c.accumulate; w.row_residual = at<float>(ws, f.row_residual);
-    w.counter = at<uint32_t>(ws, f.counters);
+    w.counter = at<uint32_t>(ws, f.counters); w.two_terms = at<int32_t>(ws, f.two_terms);
     if ((e = encode_matrix_map(&w.x_k, c.x, c.rows, c.hidden, c.x_stride * 2, ceil_div(c.rows, 16) * 16, 64, false)) != cudaSuccess ||
         (e = encode_matrix_map(&w.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, 128, 64, false)) != cudaSuccess)
       return e;
     int ctas = 0;
     if ((e = launch_few<true>(w, sm_count, &ctas, stream)) != cudaSuccess || !products) return e;
     const int words = ceil_div(c.vocab, 128) * 128;
-    if ((e = encode_matrix_map(&p.g_k[0], g, words, f.g_pitch, f.g_pitch * 2, kHalf, 64, false)) != cudaSuccess ||
-        (e = encode_matrix_map(&p.g_mn[0], g, words, f.g_pitch, f.g_pitch * 2, 64, 64, false)) != cudaSuccess ||
+    // (two terms to a row: the product for dx sees the first only)
+    if ((e = encode_matrix_map(&p.g_k[0], g, words, 2 * f.g_pitch, f.g_pitch * 4, kHalf, 64, false)) != cudaSuccess ||
+        (e = encode_matrix_map(&p.g_mn[0], g, words, f.g_pitch, f.g_pitch * 4, 64, 64, false)) != cudaSuccess ||
         (e = encode_matrix_map(&p.x_mn[0], gathered, f.g_pitch, c.hidden, h_stride, 64, 64, false)) != cudaSuccess)
       return e;
     p.x_mn[1] = p.x_mn[0];
     p.x_k[0] = p.w_k = p.w_mn;      // (of kind 0, which has no tiles here)
-    p.by_words = 1; p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.counter = w.counter;
+    p.by_words = 1; p.two_terms = w.two_terms; p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.counter = w.counter;
     p.range_blocks = ceil_div(ceil_div(c.vocab, 64), f.ranges);
     const int tiles = p.n_tiles * (f.ranges + ceil_div(c.vocab, kTile));
     if ((e = launch_pairs<true>(p, tiles, sm_count, stream)) != cudaSuccess || c.dx == nullptr) return e;
