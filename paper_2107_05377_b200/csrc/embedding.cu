@@ -27,8 +27,10 @@ constexpr int kSortDigitBits = 9;                     // at most
 constexpr int kSortBins = 1 << kSortDigitBits;
 constexpr int kSortMaxCluster = 16;                   // (more than the portable eight)
 // counters of every warp, totals of this CTA (two passes in turn), first places of the digits, warp sums of a scan
-constexpr int kSortSmemBytes = (kSortWarps * kSortBins + 2 * kSortBins + kSortBins + kSortWarps) * 4;
-constexpr int kSortUnroll = 8;                        // rounds of a warp whose loads are in flight at a time
+constexpr int kSortUnroll = 8;                        // rounds of a warp whose entries are in registers at a time
+constexpr int kSortAlone = 2048;                      // tokens that one CTA sorts alone, in shared memory
+constexpr int kSortCountBytes = (kSortWarps * kSortBins + 2 * kSortBins + kSortBins + kSortWarps) * 4;
+constexpr int kSortSmemBytes = kSortCountBytes + kSortAlone * 8;
 constexpr int kSumColumns = 8;                        // columns of a thread
 constexpr int kSumUnroll = 8;                         // rows asked for at a time
 constexpr int kJoinGroups = 8;                        // warps of a CTA of the join
@@ -125,15 +127,14 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_lookup_kernel(const 
 
 // ---- sort ----------------------------------------------------------------------------------------
 
-// Lanes of `active` that hold the same digit: one vote per bit.  (match.any takes some 240 clocks of the warp here: 131072 tokens on eight
-// SMs were sorted in 76 us with it and in 57 with votes.)
+// Lanes of `active` that hold the same digit: one vote per bit.  (match.any takes some 240 clocks of the warp here.)
 __device__ __forceinline__ uint32_t same_digit(uint32_t active, uint32_t digit, int bits) {
   uint32_t same = active;
 #pragma unroll
   for (int b = 0; b < kSortDigitBits; ++b) {
-    if (b < bits) {
+    if (b < bits) {                                     // (all 32 lanes vote, converged: a vote of some of them costs a warp barrier)
       const bool one = (digit >> b) & 1u;
-      const uint32_t ones = __ballot_sync(active, one);
+      const uint32_t ones = __ballot_sync(0xffffffffu, one);
       same &= one ? ones : ~ones;
     }
   }
@@ -157,6 +158,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
   uint32_t* totals = counts + kSortWarps * kSortBins;              // [pass & 1][digit]
   uint32_t* first = totals + 2 * kSortBins;                        // [digit]
   uint32_t* warp_sums = first + kSortBins;                         // [warp]
+  uint2* kept = reinterpret_cast<uint2*>(warp_sums + kSortWarps);  // the list, of one CTA alone
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_ctas = p.sort_ctas;
   grid_dependency_wait();
@@ -189,11 +191,13 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
   uint32_t* my_counts = counts + warp * kSortBins;
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * p.digit_bits;
+    // one CTA alone keeps the list in shared memory until the last pass
+    const bool alone = n_ctas == 1;
     const uint2* src = p.list[(pass + 1) & 1];
-    uint2* dst = p.list[pass & 1];
+    uint2* dst = alone && pass + 1 < p.passes ? kept : p.list[pass & 1];
     // (id, token) at place i of the list as it is before this pass
     auto entry = [&](int i) -> uint2 {
-      if (pass != 0) return __ldcg(src + i);                       // (written by the other CTAs of the cluster: not through L1)
+      if (pass != 0) return alone ? kept[i] : __ldcg(src + i);     // (written by the other CTAs of the cluster: not through L1)
       const int id = p.ids[i];
       return make_uint2(id < 0 || id >= p.vocab || id == p.padding_id ? static_cast<uint32_t>(p.vocab) : static_cast<uint32_t>(id),
                         static_cast<uint32_t>(i));
@@ -238,8 +242,8 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
       my_totals[tid] = total;
     }
     __syncwarp();
-    cluster_sync_all();
-    if (tid < bins) {
+    if (alone) all = total; else cluster_sync_all();
+    if (tid < bins && !alone) {
       uint32_t c[kSortMaxCluster];                    // (all asked for before the first is used)
 #pragma unroll
       for (int r = 0; r < kSortMaxCluster; ++r) c[r] = r < n_ctas ? ld_cluster_u32(map_to_cta(smem_u32(my_totals + tid), r)) : 0u;
@@ -268,22 +272,20 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
       if (end - begin > 32 * kSortUnroll) fetch(i0);
 #pragma unroll
       for (int u = 0; u < kSortUnroll; ++u) {
+        if (i0 + 32 * u >= end) break;                    // (the same for all lanes)
         const bool there = i0 + 32 * u + lane < end;
-        const uint32_t active = __ballot_sync(0xffffffffu, there);
-        if (there) {
-          const uint32_t digit = (e[u].x >> shift) & (bins - 1);
-          const uint32_t same = same_digit(active, digit, p.digit_bits);
-          const uint32_t place = first[digit] + my_counts[digit] + __popc(same & ((1u << lane) - 1));
-          __syncwarp(active);
-          if (lane == __ffs(same) - 1) my_counts[digit] += __popc(same);
-          dst[place] = e[u];
-        }
+        const uint32_t digit = (e[u].x >> shift) & (bins - 1);
+        const uint32_t same = same_digit(__ballot_sync(0xffffffffu, there), digit, p.digit_bits);
+        const uint32_t place = first[digit] + my_counts[digit] + __popc(same & ((1u << lane) - 1));
+        __syncwarp();
+        if (there && lane == __ffs(same) - 1) my_counts[digit] += __popc(same);
+        if (there) dst[place] = e[u];
         __syncwarp();
       }
     }
     // the next pass reads what the other CTAs have written (and no CTA leaves while another reads its totals)
     __syncwarp();
-    cluster_sync_all();
+    if (alone) __syncthreads(); else cluster_sync_all();
   }
 }
 
@@ -689,11 +691,12 @@ cudaError_t launch_sort(EmbeddingGradParams* p, int sm_count, cudaStream_t strea
     return cudaSuccess;
   }, &device);
   if (err != cudaSuccess) return err;
-  // A CTA of the cluster per round of all its warps, as far as sixteen of them (where so many fit; else eight).  What a pass costs is
-  // its stores, 32 places per warp that lie anywhere: one per clock and SM.  131072 tokens: 76 us with match.any and ids and tokens
-  // stored apart, eight CTAs; 57 with votes; 28 with one store for both, sixteen CTAs and the entries kept in registers.
+  // Up to 2048 tokens one CTA: no trip between CTAs nor to L2 between the passes (2048 tokens 10 us against 12 with two CTAs; 4096 14 against
+  // 12).  Beyond, a CTA of the cluster per round of all its warps, as far as sixteen of them (where so many fit; else eight): what a pass
+  // costs then is the issue of the votes and of stores to 32 places per warp.  131072 tokens: 76 us with match.any, ids and tokens stored
+  // apart and eight CTAs; 57 with votes; 26 with one store for both, sixteen CTAs, entries kept in registers and all lanes voting.
   int ctas = 1;
-  while (ctas < most_ctas[device] && static_cast<int64_t>(ctas) * kSortThreads < p->tokens) ctas *= 2;
+  while (p->tokens > kSortAlone && ctas < most_ctas[device] && static_cast<int64_t>(ctas) * kSortThreads < p->tokens) ctas *= 2;
   p->sort_ctas = ctas;
   int fill = 0;
   if (!p->accumulate) {

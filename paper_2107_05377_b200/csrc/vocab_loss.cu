@@ -1134,14 +1134,21 @@ constexpr int kSharedUnits = 1024;
 
 // A warp per row: log-sum-exp and loss from (largest logit, sum) of every half tile.
 __global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __grid_constant__ VocabJoinParams p) {
+  const int lane = threadIdx.x & 31;
+  const int step = gridDim.x * (kJoinThreads / 32);
+  int row = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+  // The kernel before this one (the product) has waited for all before it and lets this one start after that: labels, places and the count
+  // are complete when this kernel begins.
+  const int rows = p.count != nullptr ? min(p.rows, __ldcg(p.count)) : p.rows;
+  int label = row < rows ? __ldcg(p.labels + row) : 0, to = row;
+  if (p.row_of != nullptr && row < rows) to = __ldcg(p.row_of + row);
   grid_dependency_wait();
   grid_launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const int rows = p.count != nullptr ? min(p.rows, *reinterpret_cast<const volatile int*>(p.count)) : p.rows;
-  const int step = gridDim.x * (kJoinThreads / 32);
-  for (int row = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); row < rows; row += step) {
-    const int label = p.labels[row];
-    const int to = p.row_of != nullptr ? p.row_of[row] : row;
+  for (bool first = true; row < rows; row += step, first = false) {
+    if (!first) {
+      label = p.labels[row];
+      to = p.row_of != nullptr ? p.row_of[row] : row;
+    }
     if (label < 0 || label >= p.vocab) {             // (only where the rows were not gathered)
       if (lane == 0) {
         if (label >= p.vocab && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
@@ -1178,10 +1185,10 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __g
 __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid_constant__ VocabFinishParams p) {
   __shared__ float s_sum[kJoinThreads / 32][32];
   __shared__ float s_acc[kJoinThreads / 32][8][32];
-  grid_dependency_wait();
-  grid_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (static_cast<int>(blockIdx.x) < p.db_ctas) {
+    grid_dependency_wait();
+    grid_launch_dependents();
     const int blocks = (__ldcg(&p.work->rows) + 31) / 32;
     const int col = blockIdx.x * 32 + lane;
     float sum = 0.f;
@@ -1206,13 +1213,28 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid
   const int share = shared ? kJoinThreads / 32 : 1;
   const int64_t step = static_cast<int64_t>(gridDim.x - p.db_ctas) * (shared ? 1 : kJoinThreads / 32);
   const int64_t cta = blockIdx.x - p.db_ctas;
+  // Only the sums come from the kernel before this one, which has waited for all before it: the rest of a first unit is fetched before the
+  // wait.
+  bool waited = false;
   for (int64_t u = shared ? cta : cta * (kJoinThreads / 32) + warp; u < units; u += step) {
     const int row = static_cast<int>(u / blocks), c = static_cast<int>(u % blocks) * 256 + lane * 8;
     const bool inside = c < p.hidden;
-    const int label = p.labels[row];
-    const int place = p.place_of != nullptr ? p.place_of[row] : row;
+    const int label = __ldcg(p.labels + row);
+    const int place = p.place_of != nullptr ? __ldcg(p.place_of + row) : row;
+    const bool counts = label >= 0 && label < p.vocab;
+    uint4 word = make_uint4(0, 0, 0, 0);
+    float residual = 0.f;
+    if (counts && inside) {
+      word = __ldcg(reinterpret_cast<const uint4*>(p.w + static_cast<int64_t>(label) * p.w_stride + c));
+      residual = __ldcg(p.row_residual + place);
+    }
+    if (!waited) {
+      grid_dependency_wait();
+      grid_launch_dependents();
+      waited = true;
+    }
     bf16* out = p.dx + static_cast<int64_t>(row) * p.dx_stride + c;
-    if (label < 0 || label >= p.vocab) {                  // (the same for all who share a unit)
+    if (!counts) {                                        // (the same for all who share a unit)
       if (inside && (!shared || warp == 0)) *reinterpret_cast<uint4*>(out) = make_uint4(0, 0, 0, 0);
       continue;
     }
@@ -1221,8 +1243,6 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
     if (inside) {
       const float* src = p.sums + static_cast<int64_t>(place) * p.hidden + c;
-      const uint4 word = __ldg(reinterpret_cast<const uint4*>(p.w + static_cast<int64_t>(label) * p.w_stride + c));
-      const float residual = p.row_residual[place];
 #pragma unroll 4
       for (int s = shared ? warp : 0; s < ranges; s += share) {
         const float4* f = reinterpret_cast<const float4*>(src + s * row_pitch * p.hidden);
