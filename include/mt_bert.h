@@ -481,7 +481,7 @@ int mt_kernel_pooler_head_static(const void* d_hidden, const void* d_pool_w, con
 
 /* out[t, :] = scale * table[ids[t], :], tokens x hidden from a table [vocab, hidden], in fp32 and rounded once.  An id below 0
  * is no token (a padded batch): its row of out is zeros.  So is that of an id >= vocab, which also sets MT_FLAG_BAD_TOKEN in
- * *d_status (may be NULL).  Rows of 8 elements that are 16-byte aligned (hidden, strides multiples of 8) move fastest. */
+ * *d_status (may be NULL).  tokens <= 2^30, hidden <= 2^20.  Rows of 8 elements that are 16-byte aligned (hidden, strides multiples of 8) move fastest. */
 int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* d_out, int32_t tokens, int32_t vocab,
                                int32_t hidden, int64_t table_stride, int64_t out_stride, int32_t table_dtype,
                                int32_t out_dtype, float scale, uint32_t* d_status, void* stream);
@@ -489,7 +489,7 @@ int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* 
 /* Gradient of the table: grad_table[v, :] = scale * sum over t with ids[t] = v of grad_out[t, :], summed in fp32 in an order
  * that depends on the ids alone and rounded once; rows without a token become zeros.  accumulate != 0 adds to what grad_table
  * holds instead, and leaves rows without a token alone.  Ids below 0 or >= vocab (flagged) have no part in it, nor has
- * padding_id (< 0: there is none).  grad_out is not read at tokens that have no part.  tokens <= 2^30. */
+ * padding_id (< 0: there is none).  grad_out is not read at tokens that have no part. */
 size_t mt_kernel_embedding_grad_workspace(int32_t tokens, int32_t vocab, int32_t hidden);
 int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void* d_grad_table, int32_t tokens, int32_t vocab,
                              int32_t hidden, int64_t grad_out_stride, int64_t grad_table_stride, int32_t grad_out_dtype,
@@ -503,8 +503,8 @@ int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void*
  * of a step whose masks are to differ.  d_counter: NULL, or a device word that is added to `counter` (modulo 2^64) when the call
  * runs - a replayed CUDA graph makes a new mask every time if something on its stream advances it.  The gradient with respect to
  * x is this same call on the gradient of y, without a residual; that of the residual is the gradient of y.
- * x has x_dtype, residual and y have y_dtype; y may be x or the residual itself, with the same stride.  p = 1 gives the residual.
- * Dropped elements may be infinite or NaN. */
+ * x has x_dtype, residual and y have y_dtype; y may be x or the residual itself, with the same type and stride.  p = 1 gives the
+ * residual.  Dropped elements may be infinite or NaN.  cols <= 2^20. */
 int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_t rows, int32_t cols, int64_t x_stride,
                       int64_t residual_stride, int64_t y_stride, int32_t x_dtype, int32_t y_dtype, double p, uint64_t seed,
                       uint64_t counter, const uint64_t* d_counter, void* stream);

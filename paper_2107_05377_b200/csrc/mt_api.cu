@@ -2429,7 +2429,7 @@ int mt_kernel_pooler_head(const void* d_hidden, const void* d_pool_w, const void
 
 static bool known_dtype(int32_t dtype) { return dtype == MT_DTYPE_BF16 || dtype == MT_DTYPE_F32; }
 static bool misaligned(const void* p, int32_t dtype) { return reinterpret_cast<uintptr_t>(p) % (dtype == MT_DTYPE_F32 ? 4 : 2) != 0; }
-static constexpr int32_t kMaxTokens = 1 << 30;
+static constexpr int32_t kMaxTokens = 1 << 30, kMaxColumns = 1 << 20;   // (what the grids and 32-bit indices of a row hold)
 
 // SMs of the current device (MT_ERR_CUDA without one).
 static int current_sms(int* sms) {
@@ -2449,7 +2449,8 @@ int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* 
                                int64_t table_stride, int64_t out_stride, int32_t table_dtype, int32_t out_dtype, float scale,
                                uint32_t* d_status, void* stream) {
   if (!known_dtype(table_dtype) || !known_dtype(out_dtype)) return MT_ERR_UNSUPPORTED;
-  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || table_stride < hidden || out_stride < hidden) return MT_ERR_SHAPE;
+  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || hidden > kMaxColumns || table_stride < hidden || out_stride < hidden)
+    return MT_ERR_SHAPE;
   if (tokens == 0) return MT_OK;
   if (d_ids == nullptr || d_table == nullptr || d_out == nullptr || reinterpret_cast<uintptr_t>(d_ids) % 4 != 0 ||
       misaligned(d_table, table_dtype) || misaligned(d_out, out_dtype))
@@ -2468,7 +2469,7 @@ static size_t embedding_list_bytes(int32_t tokens) { return whole_lines(static_c
 static int64_t embedding_part_stride(int32_t hidden) { return (static_cast<int64_t>(hidden) + 7) / 8 * 8; }
 
 size_t mt_kernel_embedding_grad_workspace(int32_t tokens, int32_t vocab, int32_t hidden) {
-  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1) return 0;
+  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || hidden > kMaxColumns) return 0;
   if (tokens == 0) return 256;
   const int chunk = embedding_grad_chunk(tokens);
   const size_t chunks = (static_cast<size_t>(tokens) + chunk - 1) / chunk;
@@ -2480,7 +2481,8 @@ int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void*
                              int32_t grad_table_dtype, float scale, int32_t padding_id, int32_t accumulate, void* d_workspace,
                              size_t workspace_bytes, uint32_t* d_status, void* stream) {
   if (!known_dtype(grad_out_dtype) || !known_dtype(grad_table_dtype)) return MT_ERR_UNSUPPORTED;
-  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || grad_out_stride < hidden || grad_table_stride < hidden)
+  if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || hidden > kMaxColumns || grad_out_stride < hidden ||
+      grad_table_stride < hidden)
     return MT_ERR_SHAPE;
   if (d_grad_table == nullptr || misaligned(d_grad_table, grad_table_dtype)) return MT_ERR_INVALID_ARG;
   if (tokens > 0 && (d_ids == nullptr || d_grad_out == nullptr || reinterpret_cast<uintptr_t>(d_ids) % 4 != 0 ||
@@ -2510,7 +2512,7 @@ int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_
                       uint64_t counter, const uint64_t* d_counter, void* stream) {
   if (!known_dtype(x_dtype) || !known_dtype(y_dtype)) return MT_ERR_UNSUPPORTED;
   if (!(p_drop >= 0.0 && p_drop <= 1.0)) return MT_ERR_INVALID_ARG;
-  if (rows < 0 || cols < 0 || x_stride < cols || y_stride < cols || (d_residual != nullptr && residual_stride < cols)) return MT_ERR_SHAPE;
+  if (rows < 0 || cols < 0 || cols > kMaxColumns || x_stride < cols || y_stride < cols || (d_residual != nullptr && residual_stride < cols)) return MT_ERR_SHAPE;
   if (rows == 0 || cols == 0) return MT_OK;
   if (d_x == nullptr || d_y == nullptr || misaligned(d_x, x_dtype) || misaligned(d_y, y_dtype) || misaligned(d_residual, y_dtype) ||
       reinterpret_cast<uintptr_t>(d_counter) % 8 != 0)

@@ -7,6 +7,9 @@
     python -m paper_2107_05377_b200.kernel_bench layernorm --rows 4096 --hidden 768
     python -m paper_2107_05377_b200.kernel_bench embed --batch 256 --seq 128
     python -m paper_2107_05377_b200.kernel_bench linear_fp8 --m 4096 --n 2304 --k 768            # E4M3 operands
+    python -m paper_2107_05377_b200.kernel_bench embedding --tokens 4096 --vocab 30522         # lookup, and its gradient
+    python -m paper_2107_05377_b200.kernel_bench dropout --rows 4096 --hidden 768              # with a residual
+    python -m paper_2107_05377_b200.kernel_bench vocab_loss --rows 4096 --vocab 30522          # cross entropy, and its gradient
     python -m paper_2107_05377_b200.kernel_bench suite          # the shapes of the 32 x 128 workload
 
 Times `--iters` launches between CUDA events on the launching stream after `--warmup` launches; with
@@ -167,9 +170,46 @@ def bench_layernorm(rows, hidden, iters, warmup, flush):
             "gbytes_per_s": 10.0 * rows * hidden / ms / 1e6}
 
 
+def bench_embedding(tokens, vocab, hidden, iters, warmup, flush):
+    ids = (torch.exp(torch.rand(tokens, device="cuda") * torch.log(torch.tensor(float(vocab)))).int() - 1).clamp(0, vocab - 1)
+    table = torch.randn(vocab, hidden, device="cuda").bfloat16()
+    out = torch.empty(tokens, hidden, device="cuda", dtype=torch.bfloat16)
+    grad = torch.empty(vocab, hidden, device="cuda", dtype=torch.bfloat16)
+    ws = torch.empty(mt.mt_kernel_embedding_grad_workspace(tokens, vocab, hidden), dtype=torch.uint8, device="cuda")
+    size = {"tokens": tokens, "vocab": vocab, "hidden": hidden}
+    ms = _time(lambda: mt.mt_kernel_embedding_lookup(ids, table, out), iters, warmup, flush)
+    yield {"kernel": "embedding_lookup", **size, "us": 1e3 * ms, "gbytes_per_s": 2.0 * hidden * (tokens + min(tokens, vocab)) / ms / 1e6}
+    ms = _time(lambda: mt.mt_kernel_embedding_grad(ids, out, grad, ws), iters, warmup, flush)
+    yield {"kernel": "embedding_grad", **size, "us": 1e3 * ms, "gbytes_per_s": 2.0 * hidden * (tokens + vocab) / ms / 1e6}
+
+
+def bench_dropout(rows, hidden, iters, warmup, flush):
+    x = torch.randn(rows, hidden, device="cuda").bfloat16()
+    r, y = torch.randn(rows, hidden, device="cuda"), torch.empty(rows, hidden, device="cuda")
+    ms = _time(lambda: mt.mt_kernel_dropout(x, y, 0.1, 1, 2, residual=r), iters, warmup, flush)
+    return {"kernel": "dropout", "rows": rows, "hidden": hidden, "us": 1e3 * ms, "gbytes_per_s": 10.0 * rows * hidden / ms / 1e6}
+
+
+def bench_vocab_loss(rows, vocab, hidden, iters, warmup, flush):
+    x = torch.randn(rows, hidden, device="cuda").bfloat16()
+    w = (torch.randn(vocab, hidden, device="cuda") * hidden ** -0.5).bfloat16()
+    bias = torch.zeros(vocab, device="cuda", dtype=torch.bfloat16)
+    labels = torch.randint(0, vocab, (rows,), device="cuda", dtype=torch.int32)
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(vocab, device="cuda")
+    size = {"rows": rows, "vocab": vocab, "hidden": hidden}
+    ws = torch.empty(mt.mt_kernel_vocab_loss_workspace(rows, vocab, hidden), dtype=torch.uint8, device="cuda")
+    ms = _time(lambda: mt.mt_kernel_vocab_loss(x, w, bias, labels, loss, lse, ws), iters, warmup, flush)
+    yield {"kernel": "vocab_loss", **size, "us": 1e3 * ms, "tflops": 2.0 * rows * vocab * hidden / ms / 1e9}
+    ws = torch.empty(mt.mt_kernel_vocab_loss_grad_workspace(rows, vocab, hidden), dtype=torch.uint8, device="cuda")
+    ms = _time(lambda: mt.mt_kernel_vocab_loss_grad(x, w, bias, labels, lse, None, dx, dw, db, ws), iters, warmup, flush)
+    yield {"kernel": "vocab_loss_grad", **size, "us": 1e3 * ms, "tflops": 6.0 * rows * vocab * hidden / ms / 1e9}
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("kernel", choices=["linear", "linear_fp8", "linear_ln", "attention", "layernorm", "embed", "suite"])
+    ap.add_argument("kernel", choices=["linear", "linear_fp8", "linear_ln", "attention", "layernorm", "embed", "embedding", "dropout", "vocab_loss",
+                                       "suite"])
     ap.add_argument("--m", type=int, default=4096)
     ap.add_argument("--n", type=int, default=2304)
     ap.add_argument("--k", type=int, default=768)
@@ -180,6 +220,8 @@ def main():
     ap.add_argument("--len-lo", type=int, default=16)
     ap.add_argument("--rows", type=int, default=4096)
     ap.add_argument("--hidden", type=int, default=768)
+    ap.add_argument("--tokens", type=int, default=4096)
+    ap.add_argument("--vocab", type=int, default=30522)
     ap.add_argument("--iters", type=int, default=50)
     ap.add_argument("--warmup", type=int, default=5)
     ap.add_argument("--flush", action="store_true")
@@ -208,6 +250,14 @@ def main():
         print(json.dumps(bench_layernorm(a.rows, a.hidden, a.iters, a.warmup, a.flush)))
     elif a.kernel == "embed":
         print(json.dumps(bench_embed(a.batch, a.seq, a.hidden, a.iters, a.warmup, a.flush)))
+    elif a.kernel == "embedding":
+        for line in bench_embedding(a.tokens, a.vocab, a.hidden, a.iters, a.warmup, a.flush):
+            print(json.dumps(line))
+    elif a.kernel == "dropout":
+        print(json.dumps(bench_dropout(a.rows, a.hidden, a.iters, a.warmup, a.flush)))
+    elif a.kernel == "vocab_loss":
+        for line in bench_vocab_loss(a.rows, a.vocab, a.hidden, a.iters, a.warmup, a.flush):
+            print(json.dumps(line))
     else:
         for m in (2409, 4096, 24576):   # the valid tokens of the 32 x 128 batch, its padded rows, six layers of them
             for (n, k, e) in ((2304, 768, 0), (768, 768, 2), (3072, 768, 1), (768, 3072, 2)):

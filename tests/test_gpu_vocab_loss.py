@@ -177,6 +177,44 @@ def test_accumulation(rows, vocab):
     check_backward(c, out, f64(lse), old)
 
 
+@pytest.mark.parametrize("rows", [1, 100, 129, 300, 4100])
+def test_weights_of_any_sign(rows):
+    """Weights below zero, zero (their rows have no gradient), tiny and huge ones."""
+    c = Case(rows, 2100, 72, True, 0.1)
+    c.dloss[::3] *= -1.0
+    c.dloss[1::5] = 0.0
+    c.dloss[2::7] *= 1e-12
+    c.dloss[4::11] *= 1e6
+    c.dev_dloss = c.dloss.cuda()
+    lse = c.forward()[1]
+    out, _, _ = c.backward(lse)
+    torch.cuda.synchronize()
+    check_backward(c, out, f64(lse))
+    assert not out[0][1::5].any()
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(40, 600, 4096), (300, 513, 2056), (129, 70000, 8), (128, 70000, 8)])
+def test_wide_hidden_states_and_long_vocabularies(rows, vocab, hidden):
+    c = Case(rows, vocab, hidden, True, 0.2)
+    loss, lse, _ = c.forward()
+    check_forward(c, loss, lse)
+    out, _, _ = c.backward(lse)
+    torch.cuda.synchronize()
+    check_backward(c, out, f64(lse))
+
+
+@pytest.mark.parametrize("rows", [77, 900])
+def test_the_same_label_everywhere(rows):
+    c = Case(rows, 3000, 64, False)
+    c.labels[:] = 2999
+    c.dev_labels = c.labels.cuda()
+    loss, lse, _ = c.forward()
+    check_forward(c, loss, lse)
+    out, _, _ = c.backward(lse)
+    torch.cuda.synchronize()
+    check_backward(c, out, f64(lse))
+
+
 def test_weights_of_one():
     c = Case(33, 500, 64)
     lse = c.forward()[1]
@@ -229,9 +267,10 @@ def test_labels_outside_the_vocabulary_are_flagged_and_take_no_part(rows):
     check_backward(c, out, f64(lse))
 
 
-def test_banned_words_and_sharp_rows():
+@pytest.mark.parametrize("rows", [70, 300, 4100])
+def test_banned_words_and_sharp_rows(rows):
     """A bias of -inf; whole tiles of it; logits far apart (one word has all of the probability)."""
-    c = Case(70, 1500, 64, True, 0.0, std=8.0)
+    c = Case(rows, 1500, 64, True, 0.0, std=8.0)
     c.b[200:900] = float("-inf")
     c.b[1499] = float("-inf")
     c.labels[c.b.cpu()[c.labels.long()] < -1e30] = 10

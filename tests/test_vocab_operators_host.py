@@ -27,7 +27,7 @@ def call(lib, name, base, **change):
 
 @pytest.mark.parametrize("change,want", [
     (dict(table_dtype=2), UNSUPPORTED), (dict(out_dtype=-1), UNSUPPORTED), (dict(tokens=-1), SHAPE), (dict(tokens=(1 << 30) + 1), SHAPE),
-    (dict(vocab=0), SHAPE), (dict(hidden=0), SHAPE), (dict(table_stride=15), SHAPE), (dict(out_stride=-16), SHAPE), (dict(ids=0), INVALID),
+    (dict(vocab=0), SHAPE), (dict(hidden=0), SHAPE), (dict(hidden=1 << 21, table_stride=1 << 21, out_stride=1 << 21), SHAPE), (dict(table_stride=15), SHAPE), (dict(out_stride=-16), SHAPE), (dict(ids=0), INVALID),
     (dict(table=0), INVALID), (dict(out=0), INVALID), (dict(ids=A + 2), INVALID), (dict(table=A + 1), INVALID), (dict(out=A + 2), INVALID),
     (dict(tokens=0, ids=0, table=0, out=0), 0)])
 def test_lookup(lib, change, want):
@@ -55,7 +55,7 @@ def test_gradient_workspace(lib):
 
 @pytest.mark.parametrize("change,want", [
     (dict(x_dtype=2), UNSUPPORTED), (dict(y_dtype=-3), UNSUPPORTED), (dict(p=-0.01), INVALID), (dict(p=1.01), INVALID), (dict(p=float("nan")), INVALID),
-    (dict(rows=-1), SHAPE), (dict(cols=-1), SHAPE), (dict(x_stride=15), SHAPE), (dict(y_stride=0), SHAPE), (dict(residual=A, residual_stride=4), SHAPE),
+    (dict(rows=-1), SHAPE), (dict(cols=-1), SHAPE), (dict(cols=1 << 21, x_stride=1 << 21, y_stride=1 << 21), SHAPE), (dict(x_stride=15), SHAPE), (dict(y_stride=0), SHAPE), (dict(residual=A, residual_stride=4), SHAPE),
     (dict(x=0), INVALID), (dict(y=0), INVALID), (dict(x=A + 1), INVALID), (dict(y=A + 2), INVALID), (dict(residual=A + 2, residual_stride=16), INVALID),
     (dict(counter_dev=A + 4), INVALID), (dict(rows=0, x=0, y=0), 0), (dict(cols=0, x=0, y=0), 0)])
 def test_dropout(lib, change, want):
