@@ -3,8 +3,7 @@
 //   lookup:    out[t, :]   = scale * table[id_t, :]
 //   gradient:  d_table[v, :] (+)= scale * sum over t with id_t = v of d_out[t, :]
 //
-// Both move bytes and compute next to nothing.  The lookup is one pass: a warp per token, 16-byte accesses, up to four of them in
-// flight per lane.  The gradient adds up rows in an order that depends on the ids alone, so that equal calls give equal bits: the
+// Both move bytes and compute next to nothing.  The lookup is one pass: a warp per token, 16-byte accesses.  The gradient adds up rows in an order that depends on the ids alone, so that equal calls give equal bits: the
 // tokens are sorted by id (stably), every run of equal ids is summed in order of the tokens in fp32, and rounded once.
 //
 // Up to 1024 tokens one launch does it all (embedding_grad_few_kernel).  More:
@@ -90,8 +89,9 @@ __device__ __forceinline__ void add_present8(const T* p, int n, float (&f)[8]) {
 
 // ---- lookup --------------------------------------------------------------------------------------
 
-constexpr int kLookupThreads = 256;
-constexpr int kLookupUnroll = 4;
+constexpr int kLookupThreads = 128;
+constexpr int kLookupUnroll = 2;
+constexpr int64_t kLookupMaxCtas = 1 << 24;
 
 template <typename T, typename O, bool VEC>
 __global__ void __launch_bounds__(kLookupThreads) embedding_lookup_kernel(const __grid_constant__ LookupParams p) {
@@ -636,9 +636,10 @@ __global__ void __launch_bounds__(32 * kJoinGroups) embedding_grad_few_kernel(co
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 template <typename T, typename O>
-cudaError_t launch_lookup_types(const LookupParams& p, bool vec, int sm_count, cudaStream_t stream) {
+cudaError_t launch_lookup_types(const LookupParams& p, bool vec, cudaStream_t stream) {
+  // A warp per row and no loop over rows: 130304 rows of 1024 from an fp32 table onto bf16 58.5 us; eight CTAs per SM that loop 65.6.
   const int64_t ctas = (static_cast<int64_t>(p.tokens) + kLookupThreads / 32 - 1) / (kLookupThreads / 32);
-  const int grid = static_cast<int>(ctas < 8 * sm_count ? ctas : 8 * sm_count);
+  const int grid = static_cast<int>(ctas < kLookupMaxCtas ? ctas : kLookupMaxCtas);
   return launch_kernel(vec ? embedding_lookup_kernel<T, O, true> : embedding_lookup_kernel<T, O, false>, dim3(grid), dim3(kLookupThreads), 0, stream, p);
 }
 
@@ -711,10 +712,10 @@ cudaError_t launch_sort(EmbeddingGradParams* p, int sm_count, cudaStream_t strea
 
 }  // namespace
 
-cudaError_t launch_embedding_lookup(const LookupParams& p, bool table_f32, bool out_f32, int sm_count, cudaStream_t stream) {
+cudaError_t launch_embedding_lookup(const LookupParams& p, bool table_f32, bool out_f32, cudaStream_t stream) {
   const bool vec = p.hidden % 8 == 0 && p.table_stride % 8 == 0 && p.out_stride % 8 == 0 && aligned16(p.table) && aligned16(p.out);
-  if (table_f32) return out_f32 ? launch_lookup_types<float, float>(p, vec, sm_count, stream) : launch_lookup_types<float, bf16>(p, vec, sm_count, stream);
-  return out_f32 ? launch_lookup_types<bf16, float>(p, vec, sm_count, stream) : launch_lookup_types<bf16, bf16>(p, vec, sm_count, stream);
+  if (table_f32) return out_f32 ? launch_lookup_types<float, float>(p, vec, stream) : launch_lookup_types<float, bf16>(p, vec, stream);
+  return out_f32 ? launch_lookup_types<bf16, float>(p, vec, stream) : launch_lookup_types<bf16, bf16>(p, vec, stream);
 }
 
 // Entries of a chunk: at least one round of loads; more where the list is long, so that 16 CTAs for each of 148 SMs have one chunk

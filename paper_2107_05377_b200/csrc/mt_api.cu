@@ -2455,12 +2455,10 @@ int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* 
   if (d_ids == nullptr || d_table == nullptr || d_out == nullptr || reinterpret_cast<uintptr_t>(d_ids) % 4 != 0 ||
       misaligned(d_table, table_dtype) || misaligned(d_out, out_dtype))
     return MT_ERR_INVALID_ARG;
-  int sms = 0;
-  if (current_sms(&sms) != MT_OK) return MT_ERR_CUDA;
   LookupParams p;
   p.ids = d_ids; p.table = d_table; p.out = d_out; p.table_stride = table_stride; p.out_stride = out_stride;
   p.tokens = tokens; p.vocab = vocab; p.hidden = hidden; p.scale = scale; p.status = d_status;
-  return launch_embedding_lookup(p, table_dtype == MT_DTYPE_F32, out_dtype == MT_DTYPE_F32, sms, as_stream(stream)) == cudaSuccess
+  return launch_embedding_lookup(p, table_dtype == MT_DTYPE_F32, out_dtype == MT_DTYPE_F32, as_stream(stream)) == cudaSuccess
              ? MT_OK : MT_ERR_CUDA;
 }
 
@@ -2517,8 +2515,6 @@ int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_
   if (d_x == nullptr || d_y == nullptr || misaligned(d_x, x_dtype) || misaligned(d_y, y_dtype) || misaligned(d_residual, y_dtype) ||
       reinterpret_cast<uintptr_t>(d_counter) % 8 != 0)
     return MT_ERR_INVALID_ARG;
-  int sms = 0;
-  if (current_sms(&sms) != MT_OK) return MT_ERR_CUDA;
   DropoutParams p;
   memset(&p, 0, sizeof(p));
   p.x = d_x; p.residual = d_residual; p.y = d_y;
@@ -2526,7 +2522,7 @@ int mt_kernel_dropout(const void* d_x, const void* d_residual, void* d_y, int32_
   p.rows = rows; p.cols = cols; p.seed = seed; p.counter = counter; p.counter_dev = d_counter;
   p.threshold = static_cast<uint32_t>(nearbyint(p_drop * 65536.0));      // (halves to the even neighbour)
   p.factor = p.threshold == 65536u ? 0.f : static_cast<float>(65536.0 / (65536.0 - p.threshold));
-  return launch_dropout(p, x_dtype == MT_DTYPE_F32, y_dtype == MT_DTYPE_F32, sms, as_stream(stream)) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+  return launch_dropout(p, x_dtype == MT_DTYPE_F32, y_dtype == MT_DTYPE_F32, as_stream(stream)) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 
 size_t mt_kernel_vocab_loss_workspace(int32_t rows, int32_t vocab, int32_t hidden) {

@@ -402,7 +402,7 @@ struct LookupParams {
   float scale;
   uint32_t* status;
 };
-cudaError_t launch_embedding_lookup(const LookupParams& p, bool table_f32, bool out_f32, int sm_count, cudaStream_t stream);
+cudaError_t launch_embedding_lookup(const LookupParams& p, bool table_f32, bool out_f32, cudaStream_t stream);
 
 // grad_table[v, :] (+)= scale * sum over ids[t] = v of grad_out[t, :]; up to three launches (sort, sum, join).
 constexpr int kEmbeddingMaxChunk = 1024;   // sorted entries of a CTA of the sum, at most
@@ -440,7 +440,7 @@ struct DropoutParams {
   uint64_t seed, counter;
   const uint64_t* counter_dev;   // or null: added to `counter`
 };
-cudaError_t launch_dropout(const DropoutParams& p, bool x_f32, bool y_f32, int sm_count, cudaStream_t stream);
+cudaError_t launch_dropout(const DropoutParams& p, bool x_f32, bool y_f32, cudaStream_t stream);
 
 // Tensor map of a row-major matrix [rows, cols], row_bytes from one row to the next (a multiple of 16), in boxes of box_rows x
 // box_cols whose rows are 128 bytes, with the 128-byte swizzle.
