@@ -495,8 +495,7 @@ struct VocabLossParams {
   const int32_t* labels;       // of the rows in use
   const int32_t* count;        // forward: rows in use (or null: rows)
   const VocabWork* work;       // backward, of this launch (null: few rows, all of it as given below)
-  const float* row_shift;      // backward: log2 |weight| - lse log2 e
-  const float* row_weight;
+  const float4* row_shift;     // backward, of every row: its part of the exponent in two terms, its weight
   float* row_residual;         // backward: what rounding takes from the label's entry of g
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
   float2* parts;
@@ -551,8 +550,7 @@ struct VocabRowsParams {
   int32_t* row_of;             // caller's row of a row in use
   int32_t* place_of;           // the other way round (-1: none), or null
   int32_t* row_label;
-  float* row_shift;            // backward: see VocabLossParams
-  float* row_weight;
+  float4* row_shift;           // backward: see VocabLossParams
   bf16* gathered;
   float* loss_out;             // forward: zeros for rows without a label
   float* lse_out;

@@ -470,12 +470,11 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
       const int row = m0 + lane;
       const bool row_counts = row < rows;
       int label = -1;
-      float shift2 = 0.f, weight = 0.f;
+      float4 shift = make_float4(0.f, 0.f, 0.f, 0.f);
       if (t.kind == 0 && row_counts) {
         label = p.labels[row];
         if (GRAD) {
-          shift2 = p.row_shift[row];
-          weight = p.row_weight[row];
+          shift = p.row_shift[row];
         }
       }
       if (t.kind == 0 && p.bias != nullptr && lane < 4) {   // the tile's bias, a line per 64 columns, on its way while the tile is computed
@@ -543,12 +542,11 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
 #pragma unroll
           for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(v[j]);
           add_bias(p.bias, bias, g);
-          // |weight| exp(z - lse): the weight is in the exponent
 #pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, shift2));
-          if (__any_sync(0xffffffffu, weight < 0.f)) {
+          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, shift.x) + shift.y);
+          if (__any_sync(0xffffffffu, shift.z < 0.f)) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] = weight < 0.f ? -g[j] : g[j];
+            for (int j = 0; j < 32; ++j) g[j] = shift.z < 0.f ? -g[j] : g[j];
           }
           const int at = label - col;
           const bool hit = __any_sync(0xffffffffu, at >= 0 && at < 32);
@@ -557,7 +555,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
               if (j == at) {
-                g[j] -= weight;
+                g[j] -= shift.z;
                 mine = g[j];
               }
             }
@@ -680,8 +678,13 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
   }
 }
 
-// A row's part of the exponent of weight exp(z - lse), in powers of two (the sign of the weight is put in afterwards), and its weight.
-__device__ __forceinline__ float2 weighted_shift(float lse, float weight) { return make_float2(log2f(fabsf(weight)) - lse * kLog2e, weight); }
+// What a row's entries of g need: |weight| exp(z - lse) = 2^((z log2 e + x) + y), and the weight, whose sign is put in afterwards.  -lse log2 e
+// is held in two parts, the second with the weight's logarithm, so that what is rounded is the size of the exponent and not of its terms
+// (lse is 10 and more, and a row's error would be the same in all of its entries).
+__device__ __forceinline__ float4 weighted_shift(float lse, float weight) {
+  const float high = lse * kLog2e;
+  return make_float4(-high, log2f(fabsf(weight)) - fmaf(lse, kLog2e, -high), weight, 0.f);
+}
 
 // ---- few rows ------------------------------------------------------------------------------------
 
@@ -740,10 +743,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * kFewMaxStages + 4 + 8));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_label = reinterpret_cast<int*>(book + 512);                    // of every row; -1 where it takes no part
-  float2* s_row = reinterpret_cast<float2*>(book + 512 + 512);          // (backward) weighted_shift
-  float2* s_part = reinterpret_cast<float2*>(book + 512 + 512 + 1024);  // (forward) [quarter][row]
+  float4* s_row = reinterpret_cast<float4*>(book + 512 + 512);          // (backward) weighted_shift
+  float2* s_part = reinterpret_cast<float2*>(book + 512 + 512 + 2048);  // (forward) [quarter][row]
   float* s_db = reinterpret_cast<float*>(s_part);                       // (backward) [accumulator][quarter][word]
-  static_assert(8 * (2 * kFewMaxStages + 12) + 8 <= 512 && 512 + 512 + 1024 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
+  static_assert(8 * (2 * kFewMaxStages + 12) + 8 <= 512 && 512 + 512 + 2048 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int stages = p.stages, stage_bytes = p.stage_bytes;
@@ -838,7 +841,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
       if (label >= p.vocab) label = -1;
       s_label[first] = label;
       if (GRAD)
-        s_row[first] = label >= 0 ? weighted_shift(p.lse[first], p.grad_loss != nullptr ? p.grad_loss[first] : 1.f) : make_float2(0.f, 0.f);
+        s_row[first] = label >= 0 ? weighted_shift(p.lse[first], p.grad_loss != nullptr ? p.grad_loss[first] : 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     // (the epilogue warps; nothing that can give up comes before it)
     asm volatile("bar.sync 1, %0;" ::"n"(32 * kFewWarps) : "memory");
@@ -912,8 +915,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
         } else {
           const uint32_t counts = __ballot_sync(0xffffffffu, my_label >= 0);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = ex2_approx(fmaf(z[j], kLog2e, s_row[i * 32 + j].x));
-          const uint32_t negative = __ballot_sync(0xffffffffu, s_row[i * 32 + lane].y < 0.f);
+          for (int j = 0; j < 32; ++j) {
+            const float2 shift = *reinterpret_cast<const float2*>(&s_row[i * 32 + j]);
+            z[j] = ex2_approx(fmaf(z[j], kLog2e, shift.x) + shift.y);
+          }
+          const uint32_t negative = __ballot_sync(0xffffffffu, s_row[i * 32 + lane].z < 0.f);
           if (negative != 0) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) z[j] = ((negative >> j) & 1u) ? -z[j] : z[j];
@@ -922,7 +928,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
               if (((hits >> j) & 1u) && s_label[i * 32 + j] == word) {
-                z[j] -= s_row[i * 32 + j].y;
+                z[j] -= s_row[i * 32 + j].z;
                 p.row_residual[i * 32 + j] = z[j] - __bfloat162float(__float2bfloat16_rn(z[j]));   // what rounding takes from the label's entry
               }
             }
@@ -1093,11 +1099,7 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
       if (has) {
         p.row_of[place] = r;
         p.row_label[place] = p.labels[r];
-        if (p.row_shift != nullptr) {
-          const float2 shift = weighted_shift(p.lse[r], p.grad_loss != nullptr ? p.grad_loss[r] : 1.f);
-          p.row_shift[place] = shift.x;
-          p.row_weight[place] = shift.y;
-        }
+        if (p.row_shift != nullptr) p.row_shift[place] = weighted_shift(p.lse[r], p.grad_loss != nullptr ? p.grad_loss[r] : 1.f);
       } else if (p.loss_out != nullptr) {
         p.loss_out[r] = 0.f;
         p.lse_out[r] = 0.f;
@@ -1357,7 +1359,7 @@ struct GradPlan {
   int piece, pieces, buffers, block_h, ranges, g_pitch, max_shift;
   bool few;
   int64_t row_pitch, dx_rows;
-  size_t count, work, counters, row_of, row_label, row_shift, row_weight, row_residual, place_of, gathered, g, two_terms, dx, bias_parts, bytes;
+  size_t count, work, counters, row_of, row_label, row_shift, row_residual, place_of, gathered, g, two_terms, dx, bias_parts, bytes;
 };
 GradPlan grad_plan(int rows, int vocab, int hidden) {
   GradPlan f;
@@ -1385,8 +1387,7 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.counters = take((static_cast<size_t>(f.pieces) + 1) * 4);
   f.row_of = take(f.row_pitch * 4);
   f.row_label = take(f.row_pitch * 4);
-  f.row_shift = take(f.row_pitch * 4);
-  f.row_weight = take(f.row_pitch * 4);
+  f.row_shift = take(f.row_pitch * 16);
   f.row_residual = take(f.row_pitch * 4);
   f.place_of = take(f.row_pitch * 4);
   f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
@@ -1522,7 +1523,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   memset(&r, 0, sizeof(r));
   r.labels = c.labels; r.x = c.x; r.x_stride = c.x_stride; r.rows = c.rows; r.vocab = c.vocab; r.hidden = c.hidden;
   r.count = at<int32_t>(ws, f.count); r.row_of = at<int32_t>(ws, f.row_of); r.row_label = at<int32_t>(ws, f.row_label);
-  r.row_shift = at<float>(ws, f.row_shift); r.row_weight = at<float>(ws, f.row_weight); r.place_of = at<int32_t>(ws, f.place_of);
+  r.row_shift = at<float4>(ws, f.row_shift); r.place_of = at<int32_t>(ws, f.place_of);
   r.lse = c.lse; r.grad_loss = c.grad_loss; r.gathered = at<bf16>(ws, f.gathered);
   r.counters = at<uint32_t>(ws, f.counters); r.n_counters = f.pieces + 1; r.status = c.status;
   r.work = at<VocabWork>(ws, f.work); r.piece = f.piece; r.max_shift = f.max_shift; r.buffers = f.buffers; r.buffer_rows = static_cast<int>(f.row_pitch);
@@ -1531,7 +1532,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   launch_rows_setup(&r, &ctas);
   if ((e = launch_kernel(vocab_rows_kernel, dim3(ctas), dim3(kRowsThreads), 0, stream, r)) != cudaSuccess) return e;
 
-  p.labels = r.row_label; p.row_shift = r.row_shift; p.row_weight = r.row_weight; p.row_residual = at<float>(ws, f.row_residual);
+  p.labels = r.row_label; p.row_shift = r.row_shift; p.row_residual = at<float>(ws, f.row_residual);
   p.bias_parts = c.db != nullptr ? at<float>(ws, f.bias_parts) : nullptr; p.bias_pitch = c.vocab;
   p.g = g; p.piece = f.piece;
   if ((e = encode_matrix_map(&p.x_k[0], c.x, c.rows, c.hidden, c.x_stride * 2, kHalf, 64, false)) != cudaSuccess ||
