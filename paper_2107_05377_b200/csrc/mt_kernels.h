@@ -495,7 +495,7 @@ struct VocabLossParams {
   const int32_t* labels;       // of the rows in use
   const int32_t* count;        // forward: rows in use (or null: rows)
   const VocabWork* work;       // backward, of this launch (null: few rows, all of it as given below)
-  const float4* row_shift;     // backward, of every row: its part of the exponent in two terms, its weight
+  const float4* row_shift;     // backward, of every row: its lse, its weight's logarithm and its weight
   float* row_residual;         // backward: what rounding takes from the label's entry of g
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
   float2* parts;
@@ -548,10 +548,11 @@ struct VocabRowsParams {
   int32_t* count;
   uint32_t* counters;          // set to zero
   int32_t* row_of;             // caller's row of a row in use
-  int32_t* place_of;           // the other way round (-1: none), or null
   int32_t* row_label;
   float4* row_shift;           // backward: see VocabLossParams
   bf16* gathered;
+  bf16* dx;                    // backward: zeros for rows without a label; or null
+  int64_t dx_stride;
   float* loss_out;             // forward: zeros for rows without a label
   float* lse_out;
   uint32_t* status;
@@ -570,8 +571,8 @@ struct VocabJoinParams {
 struct VocabFinishParams {
   const VocabWork* work;       // (null: few rows, in place, ranges and row_pitch as given)
   const float* sums;           // [ranges][row_pitch][hidden]
-  const int32_t* place_of;
-  const int32_t* labels;
+  const int32_t* row_of;       // caller's row of a row in use (null: the same)
+  const int32_t* labels;       // of the rows in use
   const float* row_residual;
   const bf16* w;
   int64_t w_stride;

@@ -43,9 +43,8 @@ constexpr int kBook = 1024;
 constexpr int kSlots = 4;                  // tiles announced ahead
 constexpr uint32_t kTmemCols = 512;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaxRanges = 32;             // of the vocabulary, for dx
-constexpr float kFloor = -1e30f;           // below every logit that counts; finite, so that -inf minus it is no NaN
+constexpr float kFloor = -3.402823466e38f;  // the lowest finite number: below every logit that counts, and -inf minus it is no NaN
 
 // All of shared memory is the ring: what a pair computes is bound by how many bytes are on their way (32 KB per k-block and CTA, of the 64
 // per clock that an SM takes in), so results leave straight from registers instead of through staging buffers.  (Forward, 8192 rows x
@@ -485,7 +484,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
       tc_fence_after();
       const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc * kTile);
       if (!GRAD) {
-        float top2 = kFloor, sum = 0.f;                 // largest logit times log2 e, sum of 2^(z log2 e - top2)
+        float top = kFloor, sum = 0.f;                  // largest logit, sum of exp(z - top)
         const int n0 = t.n * p.block_n;
 #pragma unroll 1
         for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
@@ -514,15 +513,15 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
           float m = z[0];
 #pragma unroll
           for (int j = 1; j < 32; ++j) m = fmaxf(m, z[j]);
-          const float next2 = fmaxf(top2, m * kLog2e);
-          sum *= ex2_approx(top2 - next2);
-          top2 = next2;
+          const float next = fmaxf(top, m);
+          sum *= ex2_approx((top - next) * kLog2e);
+          top = next;
           float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 32; ++j) s[j & 3] += ex2_approx(fmaf(z[j], kLog2e, -top2));
+          for (int j = 0; j < 32; ++j) s[j & 3] += ex2_approx((z[j] - top) * kLog2e);   // (differences first: logits may be at the lowest number)
           sum += (s[0] + s[1]) + (s[2] + s[3]);
         }
-        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + GROUPS * t.n + group] = make_float2(top2, sum);
+        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + GROUPS * t.n + group] = make_float2(top, sum);
       } else if (t.kind == 0) {
         const int n0 = t.n * p.block_n;                 // in the piece
         const bool whole = __all_sync(0xffffffffu, row_counts);
@@ -543,7 +542,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
           for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(v[j]);
           add_bias(p.bias, bias, g);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j], kLog2e, shift.x) + shift.y);
+          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j] - shift.x, kLog2e, shift.y));
           if (__any_sync(0xffffffffu, shift.z < 0.f)) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) g[j] = shift.z < 0.f ? -g[j] : g[j];
@@ -678,13 +677,10 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
   }
 }
 
-// What a row's entries of g need: |weight| exp(z - lse) = 2^((z log2 e + x) + y), and the weight, whose sign is put in afterwards.  -lse log2 e
-// is held in two parts, the second with the weight's logarithm, so that what is rounded is the size of the exponent and not of its terms
-// (lse is 10 and more, and a row's error would be the same in all of its entries).
-__device__ __forceinline__ float4 weighted_shift(float lse, float weight) {
-  const float high = lse * kLog2e;
-  return make_float4(-high, log2f(fabsf(weight)) - fmaf(lse, kLog2e, -high), weight, 0.f);
-}
+// What a row's entries of g need: |weight| exp(z - lse) = 2^((z - lse) log2 e + log2 |weight|), and the weight, whose sign is put in
+// afterwards.  (z - lse first: what is rounded is the size of the exponent and not of its terms, in an error of its own for every entry; and
+// both may be at the lowest number.)
+__device__ __forceinline__ float4 weighted_shift(float lse, float weight) { return make_float4(lse, log2f(fabsf(weight)), weight, 0.f); }
 
 // ---- few rows ------------------------------------------------------------------------------------
 
@@ -908,16 +904,16 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
             for (int j = 0; j < 32; ++j) z[j] = -INFINITY;
           }
           const float2 part = my_part[i * 32];
-          const float next2 = fmaxf(part.x, column_max(z, lane) * kLog2e);
+          const float next = fmaxf(part.x, column_max(z, lane));
 #pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = ex2_approx(fmaf(z[j], kLog2e, -__shfl_sync(0xffffffffu, next2, j)));
-          my_part[i * 32] = make_float2(next2, part.y * ex2_approx(part.x - next2) + column_sums(z, lane));
+          for (int j = 0; j < 32; ++j) z[j] = ex2_approx((z[j] - __shfl_sync(0xffffffffu, next, j)) * kLog2e);
+          my_part[i * 32] = make_float2(next, part.y * ex2_approx((part.x - next) * kLog2e) + column_sums(z, lane));
         } else {
           const uint32_t counts = __ballot_sync(0xffffffffu, my_label >= 0);
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             const float2 shift = *reinterpret_cast<const float2*>(&s_row[i * 32 + j]);
-            z[j] = ex2_approx(fmaf(z[j], kLog2e, shift.x) + shift.y);
+            z[j] = ex2_approx(fmaf(z[j] - shift.x, kLog2e, shift.y));
           }
           const uint32_t negative = __ballot_sync(0xffffffffu, s_row[i * 32 + lane].z < 0.f);
           if (negative != 0) {
@@ -988,7 +984,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
 #pragma unroll
     for (int q = 0; q < 4; ++q) top = fmaxf(top, s_part[q * kFewRows + tid].x);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) sum += s_part[q * kFewRows + tid].y * ex2_approx(s_part[q * kFewRows + tid].x - top);
+    for (int q = 0; q < 4; ++q) sum += s_part[q * kFewRows + tid].y * ex2_approx((s_part[q * kFewRows + tid].x - top) * kLog2e);
     p.parts[tid * p.part_pitch + blockIdx.x] = make_float2(top, sum);
   }
   if (tid == 0 && *abort_flag && p.status != nullptr) atomicOr(p.status, kFlagWaitTimeout);
@@ -1095,7 +1091,6 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
     s_place[tid] = has ? place : -1;
     if (r < last) {
       if (p.labels[r] >= p.vocab && p.status != nullptr) atomicOr(p.status, kFlagBadToken);
-      if (p.place_of != nullptr) p.place_of[r] = has ? place : -1;
       if (has) {
         p.row_of[place] = r;
         p.row_label[place] = p.labels[r];
@@ -1110,7 +1105,13 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
       const int end = min(kRowsThreads, last - r0);
       for (int i = warp; i < end; i += kRowsThreads / 32) {
         const int to = s_place[i];
-        if (to < 0) continue;
+        if (to < 0) {
+          if (p.dx != nullptr) {
+            uint4* zeros = reinterpret_cast<uint4*>(p.dx + static_cast<int64_t>(r0 + i) * p.dx_stride);
+            for (int c = lane; c < vectors; c += 32) zeros[c] = make_uint4(0, 0, 0, 0);
+          }
+          continue;
+        }
         const uint4* src = reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(r0 + i) * p.x_stride);
         uint4* dst = reinterpret_cast<uint4*>(p.gathered + static_cast<int64_t>(to) * p.hidden);
 #pragma unroll 4
@@ -1167,22 +1168,22 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_loss_join_kernel(const __g
     float sum = 0.f;
     for (int i = lane; i < p.n_parts; i += 32) {
       const float2 part = parts[i];
-      sum += part.y * exp2f(part.x - top);
+      sum += part.y * exp2f((part.x - top) * kLog2e);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) {
       const float log_sum = logf(sum);
-      p.lse[to] = fmaf(top, kLn2, log_sum);
-      p.loss[to] = fmaf(top, kLn2, -p.label_logit[row]) + log_sum;
+      p.lse[to] = top + log_sum;
+      p.loss[to] = (top - p.label_logit[row]) + log_sum;
     }
   }
 }
 
 // The last launch of a gradient.
 // dx: the ranges of a row added up in order, and what rounding took from the label's entry of g times the label's row of W (that one entry
-// is most of a row of g: without this a row of dx would be off by its rounding); rounded once, to the row's place; zeros for rows without
-// a label.  A warp per row and 256 columns.
+// is most of a row of g: without this a row of dx would be off by its rounding); rounded once, to the caller's row.  A warp per row in use and
+// 256 columns.  (Rows without a label: zeros, from the rows' kernel, or here where the rows are in place.)
 // db (the first db_ctas CTAs): the sums of all blocks of 32 rows, in order; a CTA per 32 columns, every warp each fourth block.
 __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid_constant__ VocabFinishParams p) {
   __shared__ float s_sum[kJoinThreads / 32][32];
@@ -1210,7 +1211,8 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid
   const int64_t row_pitch = p.work != nullptr ? __ldcg(&p.work->row_pitch) : p.row_pitch;
   // With many ranges the four warps of a CTA share a unit, every fourth range each, if there are so few units that all of them run at
   // once (77 rows x 768 in 18 ranges 7.6 -> 5.1 us; 4096 x 768, 614 of them in 9 ranges, 11 -> 17).
-  const int64_t units = static_cast<int64_t>(p.rows) * blocks;
+  const int rows = p.work != nullptr ? __ldcg(&p.work->rows) : p.rows;
+  const int64_t units = static_cast<int64_t>(rows) * blocks;
   const bool shared = ranges >= 2 * kJoinThreads / 32 && units <= kSharedUnits;
   const int share = shared ? kJoinThreads / 32 : 1;
   const int64_t step = static_cast<int64_t>(gridDim.x - p.db_ctas) * (shared ? 1 : kJoinThreads / 32);
@@ -1219,10 +1221,10 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid
   // wait.
   bool waited = false;
   for (int64_t u = shared ? cta : cta * (kJoinThreads / 32) + warp; u < units; u += step) {
-    const int row = static_cast<int>(u / blocks), c = static_cast<int>(u % blocks) * 256 + lane * 8;
+    const int place = static_cast<int>(u / blocks), c = static_cast<int>(u % blocks) * 256 + lane * 8;
     const bool inside = c < p.hidden;
-    const int label = __ldcg(p.labels + row);
-    const int place = p.place_of != nullptr ? __ldcg(p.place_of + row) : row;
+    const int label = __ldcg(p.labels + place);
+    const int row = p.row_of != nullptr ? __ldcg(p.row_of + place) : place;
     const bool counts = label >= 0 && label < p.vocab;
     uint4 word = make_uint4(0, 0, 0, 0);
     float residual = 0.f;
@@ -1359,7 +1361,7 @@ struct GradPlan {
   int piece, pieces, buffers, block_h, ranges, g_pitch, max_shift;
   bool few;
   int64_t row_pitch, dx_rows;
-  size_t count, work, counters, row_of, row_label, row_shift, row_residual, place_of, gathered, g, two_terms, dx, bias_parts, bytes;
+  size_t count, work, counters, row_of, row_label, row_shift, row_residual, gathered, g, two_terms, dx, bias_parts, bytes;
 };
 GradPlan grad_plan(int rows, int vocab, int hidden) {
   GradPlan f;
@@ -1389,7 +1391,6 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.row_label = take(f.row_pitch * 4);
   f.row_shift = take(f.row_pitch * 16);
   f.row_residual = take(f.row_pitch * 4);
-  f.place_of = take(f.row_pitch * 4);
   f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
   f.g = take(static_cast<size_t>(f.buffers) * (f.few ? 2 * f.g_pitch : f.row_pitch) * f.piece * 2);
   f.two_terms = take(f.few ? static_cast<size_t>(f.piece / kTile) * 4 : 0);
@@ -1523,7 +1524,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   memset(&r, 0, sizeof(r));
   r.labels = c.labels; r.x = c.x; r.x_stride = c.x_stride; r.rows = c.rows; r.vocab = c.vocab; r.hidden = c.hidden;
   r.count = at<int32_t>(ws, f.count); r.row_of = at<int32_t>(ws, f.row_of); r.row_label = at<int32_t>(ws, f.row_label);
-  r.row_shift = at<float4>(ws, f.row_shift); r.place_of = at<int32_t>(ws, f.place_of);
+  r.row_shift = at<float4>(ws, f.row_shift); r.dx = c.dx; r.dx_stride = c.dx_stride;
   r.lse = c.lse; r.grad_loss = c.grad_loss; r.gathered = at<bf16>(ws, f.gathered);
   r.counters = at<uint32_t>(ws, f.counters); r.n_counters = f.pieces + 1; r.status = c.status;
   r.work = at<VocabWork>(ws, f.work); r.piece = f.piece; r.max_shift = f.max_shift; r.buffers = f.buffers; r.buffer_rows = static_cast<int>(f.row_pitch);
@@ -1554,7 +1555,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     if ((e = launch_pairs<true>(p, sm_count, sm_count, stream)) != cudaSuccess) return e;
   }
   if (c.dx == nullptr && c.db == nullptr) return cudaSuccess;
-  d.place_of = r.place_of; d.work = r.work; d.bias_parts = p.bias_parts; d.db_ctas = c.db != nullptr ? ceil_div(c.vocab, 32) : 0;
+  d.row_of = r.row_of; d.labels = r.row_label; d.work = r.work; d.bias_parts = p.bias_parts; d.db_ctas = c.db != nullptr ? ceil_div(c.vocab, 32) : 0;
   return launch_kernel(vocab_finish_kernel, dim3(dx_ctas + d.db_ctas), dim3(kJoinThreads), 0, stream, d);
 }
 

@@ -46,7 +46,7 @@ class Case:
         """Largest error of a logit of every row: products of bf16 numbers are exact in fp32; the sum of `hidden` of them and the
         bias is off by at most a step (the tensor cores may cut off) per addition of a partial sum below the sum of magnitudes."""
         x, w, b, _ = self.exact()
-        size = np.abs(x) @ np.abs(w).max(axis=0) + (0.0 if b is None else np.abs(b[np.isfinite(b)]).max(initial=0.0))
+        size = np.abs(x) @ np.abs(w).max(axis=0) + (0.0 if b is None else np.abs(b[b > -1e30]).max(initial=0.0))
         return (self.hidden + 2) * 2 * F32 * size
 
     def forward(self, stream=None, fill=0xFF):
@@ -284,6 +284,31 @@ def test_banned_words_and_sharp_rows(rows):
     torch.cuda.synchronize()
     check_backward(c, out, f64(lse))
     assert not out[2][200:300].any() and not out[1][301:900].any()
+
+
+@pytest.mark.parametrize("rows", [3, 70, 300, 4100])
+@pytest.mark.parametrize("left", [0, 40])
+def test_words_banned_by_the_lowest_number(rows, left):
+    """A bias of bf16's lowest value on all words but `left`: where it is on all, every logit is that value (what x and W add is lost in
+    its rounding) and the words are equally likely."""
+    c = Case(rows, 1300, 64, True, 0.1)
+    lowest = torch.finfo(torch.bfloat16).min
+    c.b[left:] = lowest
+    if left:
+        c.labels = torch.where(c.labels >= 0, c.labels % left, c.labels)
+        c.dev_labels = c.labels.cuda()
+    loss, lse, _ = c.forward()
+    out, _, _ = c.backward(lse)
+    torch.cuda.synchronize()
+    if left:
+        check_forward(c, loss, lse)
+        check_backward(c, out, f64(lse))
+        assert not out[2][left:].any() and not out[1][left:].any()
+        return
+    there = (c.labels >= 0).numpy()
+    assert (np.abs(f64(loss)[there] - np.log(1300.0)) <= 2.0 ** -18).all() and (f64(lse)[there] == float(lowest)).all()
+    # (the lse that the backward pass is given cannot hold the log 1300 above the lowest number: its probabilities are all one, but finite)
+    assert torch.isfinite(out[0]).all() and torch.isfinite(out[1]).all() and torch.isfinite(out[2]).all()
 
 
 def test_gradient_against_differences():
