@@ -285,18 +285,22 @@ cudaError_t make_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t 
 
 // Tensor map of a row-major bf16 matrix [rows, cols] as {64, rows, cols / 64}: a box is some rows of several k-blocks, one
 // behind the other in shared memory, each with the 128-byte swizzle.
-cudaError_t make_tmap_kblocks(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows, int box_kblocks) {
+cudaError_t make_tmap_kblocks_strided(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_kblocks) {
   EncodeTiledFn enc = nullptr;
   cudaError_t err = get_encoder(&enc);
   if (err != cudaSuccess) return err;
   const cuuint64_t dims[3] = {kGemmBlockK, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(cols / kGemmBlockK)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(cols) * sizeof(bf16), kGemmBlockK * sizeof(bf16)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_bytes), kGemmBlockK * sizeof(bf16)};
   const cuuint32_t box[3] = {kGemmBlockK, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(box_kblocks)};
   const cuuint32_t elem[3] = {1, 1, 1};
   CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, elem,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t make_tmap_kblocks(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows, int box_kblocks) {
+  return make_tmap_kblocks_strided(map, base, rows, cols, cols * static_cast<int64_t>(sizeof(bf16)), box_rows, box_kblocks);
 }
 
 // Tensor map of a row-major matrix [rows, cols] of bytes (E4M3 operands) accessed in boxes of box_rows x 128.
@@ -2593,5 +2597,8 @@ namespace mt {
 cudaError_t encode_matrix_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_cols,
                               bool fp32) {
   return make_tmap_strided(map, base, rows, cols, row_bytes, box_rows, box_cols, fp32);
+}
+cudaError_t encode_block_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_blocks) {
+  return make_tmap_kblocks_strided(map, base, rows, cols, row_bytes, box_rows, box_blocks);
 }
 }  // namespace mt

@@ -447,6 +447,10 @@ cudaError_t launch_dropout(const DropoutParams& p, bool x_f32, bool y_f32, cudaS
 cudaError_t encode_matrix_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_cols,
                               bool fp32);
 
+// The same matrix (bf16, cols a multiple of 64) as {64, rows, cols / 64}: a box is some rows of several blocks of 64 columns, one behind the
+// other in shared memory.
+cudaError_t encode_block_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, int box_rows, int box_blocks);
+
 // Softmax cross entropy over the vocabulary, and its gradient.  What a call is given:
 struct VocabLossCall {
   const bf16* x;
@@ -517,7 +521,7 @@ struct VocabLossParams {
 };
 // Up to 128 rows: the logits turned, words on the lanes.
 struct VocabFewParams {
-  CUtensorMap x_k, w_k;        // boxes of all rows (rounded up to 16) x 64 and of 128 x 64
+  CUtensorMap x_k, w_k;        // boxes of all rows (rounded up to 16) x 64 and of 128 x 64, or of several such blocks of columns
   const bf16* bias;
   const int32_t* labels;
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every CTA, [row][part_pitch]

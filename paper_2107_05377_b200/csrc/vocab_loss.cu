@@ -725,7 +725,7 @@ __device__ __forceinline__ float column_max(const float (&z)[32], int lane) {
   return c[0];
 }
 
-template <bool GRAD>
+template <bool GRAD, int STAGE_BLOCKS>
 __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid_constant__ VocabFewParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -747,6 +747,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int stages = p.stages, stage_bytes = p.stage_bytes;
   const int k_blocks = (p.hidden + 63) / 64;
+  constexpr uint32_t STAGE_A = STAGE_BLOCKS * kFewStageA;
   const int tiles = (p.vocab + 127) / 128;
   if (tid == 0) {
     for (int s = 0; s < kFewMaxStages; ++s) {
@@ -780,13 +781,18 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
     long long issued = 0;
     bool ok = true;
     for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-      for (int kb = 0; kb < k_blocks; ++kb) {
+      for (int kb = 0; kb < k_blocks; kb += STAGE_BLOCKS) {
         if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag))) { ok = false; break; }
         if (leader) {
           const uint32_t a = ring + stage * stage_bytes;
           mbar_expect_tx(bar_full + 8 * stage, stage_bytes);
-          tma_load_2d(a, &p.w_k, kb * 64, tile * 128, bar_full + 8 * stage);
-          tma_load_2d(a + kFewStageA, &p.x_k, kb * 64, 0, bar_full + 8 * stage);
+          if (STAGE_BLOCKS > 1) {
+            tma_load_3d(a, &p.w_k, 0, tile * 128, kb, bar_full + 8 * stage);
+            tma_load_3d(a + STAGE_A, &p.x_k, 0, 0, kb, bar_full + 8 * stage);
+          } else {
+            tma_load_2d(a, &p.w_k, kb * 64, tile * 128, bar_full + 8 * stage);
+            tma_load_2d(a + STAGE_A, &p.x_k, kb * 64, 0, bar_full + 8 * stage);
+          }
         }
         ++issued;
         if (++stage == stages) { stage = 0; phase ^= 1u; }
@@ -811,13 +817,17 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
       if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) break;
       tc_fence_after();
       const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kFewRows);
-      for (int kb = 0; kb < k_blocks; ++kb) {
+      for (int kb = 0; kb < k_blocks; kb += STAGE_BLOCKS) {
         if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
         tc_fence_after();
         if (leader) {
-          const uint64_t da = smem_desc_sw128(ring + stage * stage_bytes), db = smem_desc_sw128(ring + stage * stage_bytes + kFewStageA);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) umma_bf16(d_tmem, da + 2 * k, db + 2 * k, idesc, (kb | k) != 0 ? 1u : 0u);
+          for (int j = 0; j < STAGE_BLOCKS; ++j) {
+            const uint64_t da = smem_desc_sw128(ring + stage * stage_bytes + j * kFewStageA);
+            const uint64_t db = smem_desc_sw128(ring + stage * stage_bytes + STAGE_A + j * p.columns * 128);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) umma_bf16(d_tmem, da + 2 * k, db + 2 * k, idesc, (kb | j | k) != 0 ? 1u : 0u);
+          }
           umma_commit(bar_empty + 8 * stage);
         }
         if (++stage == stages) { stage = 0; phase ^= 1u; }
@@ -1281,21 +1291,33 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid
   }
 }
 
-template <bool GRAD>
-cudaError_t launch_few(VocabFewParams p, int sm_count, int* ctas, cudaStream_t stream) {
-  auto kernel = vocab_few_tcgen05<GRAD>;
+template <bool GRAD, int STAGE_BLOCKS>
+cudaError_t launch_few_blocks(VocabFewParams p, int sm_count, int* ctas, cudaStream_t stream) {
+  auto kernel = vocab_few_tcgen05<GRAD, STAGE_BLOCKS>;
   static PerDeviceOnce once;
   cudaError_t err = per_device_once(once, [&](int) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewRing + kFewBook + 1024);
   });
   if (err != cudaSuccess) return err;
   p.columns = (p.rows + 15) / 16 * 16;
-  p.stage_bytes = kFewStageA + p.columns * 128;
+  p.stage_bytes = STAGE_BLOCKS * (kFewStageA + p.columns * 128);
   p.stages = kFewRing / p.stage_bytes < kFewMaxStages ? kFewRing / p.stage_bytes : kFewMaxStages;
   const int tiles = (p.vocab + 127) / 128;
   *ctas = tiles < sm_count ? tiles : (sm_count > 0 ? sm_count : 1);
   if (!GRAD) p.part_pitch = *ctas;
   return launch_kernel(kernel, dim3(*ctas), dim3(kFewThreads), kFewRing + kFewBook + 1024, stream, p);
+}
+// k-blocks of a stage: a copy takes its warp some 180 clocks to issue whatever its size, and rows of W come in longer pieces.  One where the
+// width is no multiple of 64 (a map in whole blocks would reach into the next row); else three, or two with more than 32 rows, whose
+// stages of three would be too few.  (30522 x 768 with one, two, three k-blocks: 20 rows 13.9, 13.3, 12.7 us; gradient of 77 rows 45.7, 45.7, 46.5.)
+int few_stage_blocks(int rows, int hidden) { return hidden % 64 != 0 ? 1 : (rows <= 32 ? 3 : 2); }
+template <bool GRAD>
+cudaError_t launch_few(const VocabFewParams& p, int sm_count, int* ctas, cudaStream_t stream) {
+  switch (few_stage_blocks(p.rows, p.hidden)) {
+    case 3: return launch_few_blocks<GRAD, 3>(p, sm_count, ctas, stream);
+    case 2: return launch_few_blocks<GRAD, 2>(p, sm_count, ctas, stream);
+    default: return launch_few_blocks<GRAD, 1>(p, sm_count, ctas, stream);
+  }
 }
 
 template <bool GRAD>
@@ -1410,6 +1432,18 @@ T* at(void* base, size_t offset) { return reinterpret_cast<T*>(static_cast<uint8
 
 }  // namespace
 
+// The operands of the kernel for few rows.
+static cudaError_t few_maps(const VocabLossCall& c, VocabFewParams* w) {
+  const int columns = ceil_div(c.rows, 16) * 16, blocks = few_stage_blocks(c.rows, c.hidden);
+  cudaError_t e;
+  if (blocks > 1) {
+    e = encode_block_map(&w->x_k, c.x, c.rows, c.hidden, c.x_stride * 2, columns, blocks);
+    return e != cudaSuccess ? e : encode_block_map(&w->w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, 128, blocks);
+  }
+  e = encode_matrix_map(&w->x_k, c.x, c.rows, c.hidden, c.x_stride * 2, columns, 64, false);
+  return e != cudaSuccess ? e : encode_matrix_map(&w->w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, 128, 64, false);
+}
+
 size_t vocab_loss_workspace(int rows, int vocab, int hidden) { return forward_plan(rows, vocab, hidden, 148).bytes; }
 size_t vocab_loss_grad_workspace(int rows, int vocab, int hidden) { return grad_plan(rows, vocab, hidden).bytes; }
 
@@ -1422,9 +1456,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
     memset(&w, 0, sizeof(w));
     w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
     w.label_logit = at<float>(ws, f.label_logit); w.parts = at<float2>(ws, f.parts);
-    if ((e = encode_matrix_map(&w.x_k, c.x, c.rows, c.hidden, c.x_stride * 2, ceil_div(c.rows, 16) * 16, 64, false)) != cudaSuccess ||
-        (e = encode_matrix_map(&w.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, 128, 64, false)) != cudaSuccess)
-      return e;
+    if ((e = few_maps(c, &w)) != cudaSuccess) return e;
     VocabJoinParams j;
     memset(&j, 0, sizeof(j));
     if ((e = launch_few<false>(w, sm_count < kFewPartCtas ? sm_count : kFewPartCtas, &j.n_parts, stream)) != cudaSuccess) return e;
@@ -1500,9 +1532,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
     w.lse = c.lse; w.grad_loss = c.grad_loss; w.x = c.x; w.x_stride = c.x_stride; w.x_clean = c.dw != nullptr ? gathered : nullptr;
     w.g = g; w.g_pitch = f.g_pitch; w.db = c.db; w.accumulate = c.accumulate; w.row_residual = at<float>(ws, f.row_residual);
     w.counter = at<uint32_t>(ws, f.counters); w.two_terms = at<int32_t>(ws, f.two_terms);
-    if ((e = encode_matrix_map(&w.x_k, c.x, c.rows, c.hidden, c.x_stride * 2, ceil_div(c.rows, 16) * 16, 64, false)) != cudaSuccess ||
-        (e = encode_matrix_map(&w.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, 128, 64, false)) != cudaSuccess)
-      return e;
+    if ((e = few_maps(c, &w)) != cudaSuccess) return e;
     int ctas = 0;
     if ((e = launch_few<true>(w, sm_count, &ctas, stream)) != cudaSuccess || !products) return e;
     const int words = ceil_div(c.vocab, 128) * 128;
