@@ -1289,6 +1289,8 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_finish_kernel(const __grid
     if (inside)
       *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
   }
+  // (with no row in use nobody has waited: this kernel must not end before the one in front of it, whose dW the next one may read)
+  if (!waited) grid_dependency_wait();
 }
 
 template <bool GRAD, int STAGE_BLOCKS>

@@ -389,3 +389,21 @@ def test_binding_refusals():
                    dict(grad_loss=c.dev_dloss.double()), dict(lse=lse[:2]), dict(workspace=ws[:256]), dict(grad_w=out[1].cpu())]:
         with pytest.raises(mt.MTError):
             mt.mt_kernel_vocab_loss_grad(**(good | change))
+
+
+def test_what_follows_a_gradient_without_labels_sees_it_whole():
+    # no kernel of a call may end before those in front of it: the next call reads the zeros of dW at once
+    vocab, hidden, rows = 120000, 1024, 300
+    c = Case(rows, vocab, hidden, False, 2.0)
+    ws = torch.empty(mt.mt_kernel_vocab_loss_grad_workspace(rows, vocab, hidden), dtype=torch.uint8, device="cuda")
+    dx = torch.empty(rows, hidden, dtype=torch.bfloat16, device="cuda")
+    dw = torch.empty(vocab, hidden, dtype=torch.bfloat16, device="cuda")
+    lse, ids = torch.zeros(rows, device="cuda"), torch.arange(vocab, dtype=torch.int32, device="cuda")
+    seen = torch.empty(vocab, hidden, dtype=torch.bfloat16, device="cuda")
+    for _ in range(5):
+        dw.fill_(1.0)
+        seen.fill_(2.0)
+        mt.mt_kernel_vocab_loss_grad(c.x, c.w, None, c.dev_labels, lse, None, dx, dw, None, ws)
+        mt.mt_kernel_embedding_lookup(ids, dw, seen)
+        torch.cuda.synchronize()
+        assert not seen.any() and not dx.any()
