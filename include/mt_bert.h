@@ -473,7 +473,7 @@ int mt_kernel_pooler_head_static(const void* d_hidden, const void* d_pool_w, con
  * between calls, any call can be captured into a CUDA graph.  Strides count elements from one row to the next (>= the row's
  * length); rows themselves are contiguous.  A workspace is 256-byte aligned, of at least the size that its function gives, in
  * use until the stream has passed the call, and holds nothing before or after it: calls that can run at the same time need one
- * each.  Equal calls give equal bits: no sum depends on timing.
+ * each.  An output overlaps no other argument unless the call says so.  Equal calls give equal bits: no sum depends on timing.
  * Errors: UNSUPPORTED (a dtype that is none of those below), SHAPE (negative or too large sizes, strides below the row's
  * length), INVALID_ARG (null or misaligned pointers, a workspace that is too small), CUDA. */
 #define MT_DTYPE_BF16 0
