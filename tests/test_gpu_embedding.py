@@ -122,6 +122,17 @@ def test_gradient_of_one_id_only(tokens):
     grad_case(ids, 6, 64, torch.bfloat16, torch.float32)
 
 
+@pytest.mark.parametrize("hidden", [8, 260, 768, 1288, 2056, 2312])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_few_tokens_by_how_often_an_id_comes(hidden, accumulate):
+    """Ids that come once, twice ... ten times, a hundred and some hundred times among each other: rows of one block of columns to more
+    than a CTA has warps."""
+    ids = np.concatenate([np.full(k, 3 * k) for k in range(1, 11)] + [np.full(100, 40), np.full(513, 41), np.full(100, -1)])
+    ids = np.random.default_rng(hidden).permutation(ids)
+    grad_case(ids, 45, hidden, torch.bfloat16, torch.float32, accumulate=accumulate, scale=0.5)
+    grad_case(ids, 45, hidden, torch.float32, torch.bfloat16, accumulate=accumulate, padding_id=41)
+
+
 @pytest.mark.parametrize("ids", [np.full(300, -1), np.full(300, 9), np.zeros(0, np.int64)])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient_without_tokens(ids, accumulate):
