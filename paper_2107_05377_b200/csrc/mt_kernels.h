@@ -503,6 +503,7 @@ struct VocabLossParams {
   float* row_residual;         // backward: what rounding takes from the label's entry of g
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
   float2* parts;
+  float cut_off;               // part of a logit that the tensor cores lose
   float* bias_parts;           // backward: sums of g over 32 rows each, [block][bias_pitch]; or null
   bf16* g;                     // two buffers of row_pitch rows, g_pitch columns each
   float* dx_sums;              // [ranges][row_pitch][hidden]
@@ -526,6 +527,7 @@ struct VocabFewParams {
   const int32_t* labels;
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every CTA, [row][part_pitch]
   float2* parts;
+  float cut_off;
   const float* lse;            // backward
   const float* grad_loss;
   const bf16* x;

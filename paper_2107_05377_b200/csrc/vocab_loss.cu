@@ -184,6 +184,14 @@ __device__ __forceinline__ Tile find_tile(const VocabWork& w, int n_tiles, int k
   return t;
 }
 
+// A logit from its accumulator.  The tensor cores cut partial sums off towards zero, once per 16 terms; what is lost grows with the partial
+// sum, so that a logit of K terms is too small by a part K / 16 * 2^-24 / (4 ln 2) of itself on average (a step of numbers of all mantissas
+// is 1 / (2 ln 2) of 2^-23 of them, half of it is lost, and the partial sums are half the logit).  Measured on 64 to 16384 terms: 0.27 * 2^-24
+// each 16, three quarters of that.  Given back, errors of logits around 10 of 768 terms fall from 8.6e-6 to 1.5e-6, and those of db, which
+// holds differences from one, as much.
+constexpr float kCutOff = 0.27f / 16777216.f / 16.f;
+__device__ __forceinline__ float with_cut_off(uint32_t acc, float cut_off) { return fmaf(__uint_as_float(acc), cut_off, __uint_as_float(acc)); }
+
 // Bias of 32 columns from `col` on, asked for before the accumulator is waited for, and added after.
 struct Bias32 { uint4 v[4]; };
 __device__ __forceinline__ void load_bias(const bf16* bias, int col, int vocab, Bias32& b) {
@@ -497,7 +505,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
           tmem_ld_wait();
           float z[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
+          for (int j = 0; j < 32; ++j) z[j] = with_cut_off(v[j], p.cut_off);
           add_bias(p.bias, bias, z);
           if (col + 32 > p.vocab) {
 #pragma unroll
@@ -539,7 +547,7 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
           tmem_ld_wait();
           float g[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(v[j]);
+          for (int j = 0; j < 32; ++j) g[j] = with_cut_off(v[j], p.cut_off);
           add_bias(p.bias, bias, g);
 #pragma unroll
           for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j] - shift.x, kLog2e, shift.y));
@@ -896,7 +904,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
         tmem_ld_wait();
         float z[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]) + bias;
+        for (int j = 0; j < 32; ++j) z[j] = with_cut_off(v[j], p.cut_off) + bias;
         const int my_label = s_label[i * 32 + lane];                // of row i * 32 + lane
         // rows whose label is one of this warp's words
         uint32_t hits = __ballot_sync(0xffffffffu, my_label >= word0 && my_label < word0 + 32);
@@ -1456,7 +1464,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
   if (c.rows <= kFewRows) {
     VocabFewParams w;
     memset(&w, 0, sizeof(w));
-    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
+    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.cut_off = kCutOff * c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
     w.label_logit = at<float>(ws, f.label_logit); w.parts = at<float2>(ws, f.parts);
     if ((e = few_maps(c, &w)) != cudaSuccess) return e;
     VocabJoinParams j;
@@ -1478,7 +1486,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
   }
   VocabLossParams p;
   memset(&p, 0, sizeof(p));
-  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.cut_off = kCutOff * c.hidden; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
   p.labels = f.gather ? at<int32_t>(ws, f.row_label) : c.labels;
   p.count = f.gather ? at<int32_t>(ws, f.count) : nullptr;
   p.n_tiles = f.tiles_n;
@@ -1521,7 +1529,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   const bool products = c.dx != nullptr || c.dw != nullptr;
   VocabLossParams p;
   memset(&p, 0, sizeof(p));
-  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias; p.status = c.status;
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.cut_off = kCutOff * c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias; p.status = c.status;
   p.dx_sums = at<float>(ws, f.dx);
   p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate; p.n_tiles = ceil_div(c.hidden, f.block_h);
   p.dw = c.dw; p.dw_stride = c.dw_stride;
@@ -1530,7 +1538,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   if (f.few) {
     VocabFewParams w;
     memset(&w, 0, sizeof(w));
-    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
+    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.cut_off = kCutOff * c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
     w.lse = c.lse; w.grad_loss = c.grad_loss; w.x = c.x; w.x_stride = c.x_stride; w.x_clean = c.dw != nullptr ? gathered : nullptr;
     w.g = g; w.g_pitch = f.g_pitch; w.db = c.db; w.accumulate = c.accumulate; w.row_residual = at<float>(ws, f.row_residual);
     w.counter = at<uint32_t>(ws, f.counters); w.two_terms = at<int32_t>(ws, f.two_terms);

@@ -407,3 +407,21 @@ def test_what_follows_a_gradient_without_labels_sees_it_whole():
         mt.mt_kernel_embedding_lookup(ids, dw, seen)
         torch.cuda.synchronize()
         assert not seen.any() and not dx.any()
+
+
+@pytest.mark.parametrize("rows", [100, 4000])
+@pytest.mark.parametrize("hidden", [768, 4096])
+def test_logits_are_not_too_small_on_average(rows, hidden):
+    """With one word lse is the logit.  The tensor cores cut partial sums off: a logit that grows evenly over hidden / 16 of them would
+    lose about 0.27 half steps of itself each time (at most 0.5, half of it on average, and less than half a logit to lose it from)."""
+    gen = torch.Generator().manual_seed(hidden)
+    w = torch.randn(1, hidden, generator=gen) * 1.5 / hidden ** 0.5
+    x = torch.randn(rows, hidden, generator=gen) + w * (3.0 + 3.0 * torch.rand(rows, 1, generator=gen))
+    w, x = w.bfloat16().cuda(), x.bfloat16().cuda()
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    ws = torch.empty(mt.mt_kernel_vocab_loss_workspace(rows, 1, hidden), dtype=torch.uint8, device="cuda")
+    mt.mt_kernel_vocab_loss(x, w, None, torch.zeros(rows, dtype=torch.int32, device="cuda"), loss, lse, ws)
+    torch.cuda.synchronize()
+    z = (f64(x) @ f64(w).T)[:, 0]
+    assert abs((f64(lse) - z).mean()) <= 0.1 * F32 * hidden / 16 * z.mean()
+    assert not loss.any()
