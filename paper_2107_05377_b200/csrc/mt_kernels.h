@@ -485,7 +485,7 @@ struct alignas(16) VocabWork {
   int32_t shift;               // pieces are this many powers of two wider than for all rows
   int32_t row_tiles;           // tiles of 256 rows
   int32_t n0, n1, n2;          // tiles of each kind
-  int32_t k1, k2;              // k-blocks of kinds 1 (one range of the vocabulary) and 2
+  int32_t k1, k2;              // k-blocks of kinds 1 (one range of the vocabulary) and 2 (all terms of g)
   int32_t ranges;              // of a piece, that dx is summed over in
   int32_t row_pitch;           // rows in whole tiles
 };

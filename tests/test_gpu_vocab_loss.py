@@ -425,3 +425,35 @@ def test_logits_are_not_too_small_on_average(rows, hidden):
     z = (f64(x) @ f64(w).T)[:, 0]
     assert abs((f64(lse) - z).mean()) <= 0.1 * F32 * hidden / 16 * z.mean()
     assert not loss.any()
+
+
+@pytest.mark.parametrize("rows,labelled", [(60, 60), (128, 100), (129, 1), (300, 20), (300, 65), (300, 128), (4500, 40), (4500, 127), (9000, 128)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_few_labels_leave_only_the_rounding_of_the_result_in_dw(rows, labelled, accumulate):
+    """Up to 128 rows with a label, of however many: a row of dW is little else than one entry of g times a row of x, and g is taken in two
+    terms, so that its rounding (2^-8 relative, and 2^-8 of what that left) is no part of the error."""
+    vocab, hidden = 2100, 200
+    c = Case(rows, vocab, hidden, True, 0.0)
+    away = torch.randperm(rows, generator=torch.Generator().manual_seed(rows))[labelled:]
+    c.labels[away] = -1
+    c.x[away.cuda()] = float("nan")
+    c.dev_labels = c.labels.cuda()
+    x, w, b, labels = c.exact()
+    weight, there = f64(c.dloss), labels >= 0
+    _, exact_lse = orc.vocab_loss(x, w, b, labels)
+    lse = torch.from_numpy(np.where(there, exact_lse, 0.0)).float().cuda()
+    gen = torch.Generator().manual_seed(1)
+    matrix(rows, hidden, 0, gen, 1.0)
+    old = f64(matrix(vocab, hidden, 0, gen, 1e-2)[0]) if accumulate else 0.0
+    out, _, _ = c.backward(lse, accumulate=accumulate)
+    torch.cuda.synchronize()
+    want = orc.vocab_loss_grad(x, w, b, labels, weight)[1] + old
+    z = x[there] @ w.T + b
+    p = np.exp(z - exact_lse[there][:, None]) * weight[there][:, None]
+    g = p.copy()
+    g[np.arange(labelled), labels[there]] -= weight[there]
+    off = (c.logit_error()[there] + 9 * F32 * (np.abs(exact_lse[there]) + 1) + 2.0 ** -20) * 1.02
+    dg = p * off[:, None] + 4 * F32 * np.abs(g)
+    dg += BF16 ** 2 * (np.abs(g) + dg)
+    bound = dg.T @ np.abs(x[there]) + (2 * labelled + 2) * 2 * F32 * ((np.abs(g) + dg).T @ np.abs(x[there]))
+    assert (np.abs(f64(out[1]) - want) <= bound + BF16 * (np.abs(want) + bound)).all()
