@@ -503,7 +503,6 @@ struct VocabLossParams {
   float* row_residual;         // backward: what rounding takes from the label's entry of g
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
   float2* parts;
-  float cut_off;               // part of a logit that the tensor cores lose
   float* bias_parts;           // backward: sums of g over 32 rows each, [block][bias_pitch]; or null
   bf16* g;                     // two buffers of row_pitch rows, g_pitch columns each
   float* dx_sums;              // [ranges][row_pitch][hidden]
@@ -517,7 +516,7 @@ struct VocabLossParams {
   int32_t row_pitch, ranges, range_blocks;   // (few rows; k-blocks of a range)
   int32_t part_pitch, bias_pitch;
   int32_t want_x, want_w, accumulate;
-  int32_t by_words;            // g lies by words, [vocab][two terms][rows] (few rows; g_k: boxes of 128 words, g_mn: of 64)
+  // (few rows: g lies by words, [vocab][two terms][rows]; g_k: boxes of 128 words, g_mn: of 64)
   const int32_t* two_terms;    // few rows: for every 256 words, whether the second term is there; or null
 };
 // Up to 128 rows: the logits turned, words on the lanes.
@@ -527,7 +526,6 @@ struct VocabFewParams {
   const int32_t* labels;
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every CTA, [row][part_pitch]
   float2* parts;
-  float cut_off;
   const float* lse;            // backward
   const float* grad_loss;
   const bf16* x;

@@ -203,6 +203,12 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t ctas = 3
       : "memory");
 }
 
+// Registers of a thread given up or taken, by all four warps of a warpgroup; what is taken comes from what the CTA was launched with.
+template <int N>
+__device__ __forceinline__ void setmaxnreg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void setmaxnreg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 

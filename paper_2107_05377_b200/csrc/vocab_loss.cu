@@ -35,10 +35,17 @@ constexpr int kTile = 256;                 // rows and (at most) columns of a pa
 constexpr int kHalf = 128;                 // rows of a CTA
 constexpr int kStageA = kHalf * 128;       // bytes: 128 rows of 64 elements, or two boxes of 64 x 64
 constexpr int kStageB = kHalf * 128;
-// Epilogue warps: in the gradient's short tiles (few rows: two k-blocks) they are what a tile takes.
-__host__ __device__ constexpr int epilogue_warps(bool grad) { return grad ? 16 : 8; }
-__host__ __device__ constexpr int threads(bool grad) { return 32 * (2 + epilogue_warps(grad)); }
-__host__ __device__ constexpr int groups(bool grad) { return epilogue_warps(grad) / 4; }   // of the same rows: they share the columns
+// What a launch of the pair kernel is for: the forward pass, the gradient (all kinds of tiles), or the two products of few rows, whose g is
+// there.  The first two have eight epilogue warps, which keep the 128 logits that each thread has of a tile in registers; the tiles of
+// the third are so short (two k-blocks) that their epilogue is what they take, and sixteen warps share it.
+enum Mode { kForward, kGradient, kProducts };
+__host__ __device__ constexpr int epilogue_warps(Mode mode) { return mode == kProducts ? 16 : 8; }
+__host__ __device__ constexpr int first_epilogue_warp(Mode mode) { return mode == kProducts ? 2 : 4; }
+__host__ __device__ constexpr int threads(Mode mode) { return 32 * (first_epilogue_warp(mode) + epilogue_warps(mode)); }
+__host__ __device__ constexpr int groups(Mode mode) { return epilogue_warps(mode) / 4; }   // of the same rows: they share the columns
+// Registers of a thread, by warpgroup: the producer's, the MMA issuer's and the epilogue's, of the 168 that each of 384 threads starts with.
+constexpr int kIssueRegs = 56, kEpilogueRegs = 224;
+static_assert(128 * kIssueRegs + 256 * kEpilogueRegs <= 384 * 168, "within what the CTA was launched with");
 constexpr int kBook = 1024;
 constexpr int kSlots = 4;                  // tiles announced ahead
 constexpr uint32_t kTmemCols = 512;
@@ -102,10 +109,10 @@ __device__ __forceinline__ void send_words(uint32_t cluster_addr, int a, int b, 
 
 // What a launch works on: the forward pass and few rows from the arguments, otherwise as the rows' kernel has left it (without a division
 // here: every clock before the first copy counts in a short launch).
-template <bool GRAD>
+template <Mode MODE>
 __device__ __forceinline__ VocabWork load_work(const VocabLossParams& p) {
   VocabWork w;
-  if (GRAD && p.work != nullptr) {
+  if (MODE == kGradient) {
     const int4* src = reinterpret_cast<const int4*>(p.work);
     int4* dst = reinterpret_cast<int4*>(&w);
 #pragma unroll
@@ -113,9 +120,9 @@ __device__ __forceinline__ VocabWork load_work(const VocabLossParams& p) {
     return w;
   }
   w = VocabWork{};
-  w.rows = !GRAD && p.count != nullptr ? min(p.rows, __ldcg(p.count)) : p.rows;
+  w.rows = MODE == kForward && p.count != nullptr ? min(p.rows, __ldcg(p.count)) : p.rows;
   w.row_tiles = (w.rows + kTile - 1) / kTile;
-  if (!GRAD) {
+  if (MODE == kForward) {
     w.cols = p.vocab;
     w.n0 = w.row_tiles * p.n_tiles;
   } else {
@@ -189,42 +196,83 @@ __device__ __forceinline__ Tile find_tile(const VocabWork& w, int n_tiles, int k
   return t;
 }
 
-// A logit from its accumulator.  The tensor cores cut partial sums off towards zero, once per 16 terms; what is lost grows with the partial
-// sum, so that a logit of K terms is too small by a part K / 16 * 2^-24 / (4 ln 2) of itself on average (a step of numbers of all mantissas
-// is 1 / (2 ln 2) of 2^-23 of them, half of it is lost, and the partial sums are half the logit).  Measured on 64 to 16384 terms: 0.27 * 2^-24
-// each 16, three quarters of that.  Given back, errors of logits around 10 of 768 terms fall from 8.6e-6 to 1.5e-6, and those of db, which
-// holds differences from one, as much.
-constexpr float kCutOff = 0.27f / 16777216.f / 16.f;
-__device__ __forceinline__ float with_cut_off(uint32_t acc, float cut_off) { return fmaf(__uint_as_float(acc), cut_off, __uint_as_float(acc)); }
+// Logits.  The tensor cores cut partial sums off towards zero, once per instruction of 16 terms, so that a logit of dense operands that is
+// summed in one go is too small by some 0.27 * 2^-24 of itself for every 16 terms (measured on 64 to 16384 terms).  Sums are therefore made of
+// at most this many k-blocks, each in an accumulator of its own, and joined in fp32, rounding to nearest, by the epilogue: what is cut off
+// is that of a logit of 256 (forward, up to 768 wide) or 384 terms whatever the width, and a sum that fp32 holds exactly comes out exactly.
+// Each further sum costs its tile a change of accumulators and a pass over one of them, some 1300 clocks, of which a wide tile hides most.
+// (Against one sum per tile: forward, 8192 rows x 30522 x 1024 in three sums 367 -> 385 us, 4096 x 768 in three 150 -> 173; gradient, 8192 x 1024 in
+// three 1340 -> 1372, 4096 x 768 in two 555 -> 588.  In sums of four k-blocks 1024 wide took 437 and 1417 us.)
+__host__ __device__ constexpr int sum_blocks(bool grad, int k_blocks) { return !grad && k_blocks <= 12 ? 4 : 6; }
 
-// Bias of 32 columns from `col` on, asked for before the accumulator is waited for, and added after.
-struct Bias32 { uint4 v[4]; };
-__device__ __forceinline__ void load_bias(const bf16* bias, int col, int vocab, Bias32& b) {
-  if (bias == nullptr) return;
-  if (col + 32 <= vocab) {
+// A sum of 32 columns from its accumulator, and one added to what is there.
+__device__ __forceinline__ void take_sum(float (&z)[32], uint32_t taddr) {
+  uint32_t v[32];
+  tmem_ld_32x32(taddr, v);
+  tmem_ld_wait();
 #pragma unroll
-    for (int q = 0; q < 4; ++q) b.v[q] = __ldg(reinterpret_cast<const uint4*>(bias + col) + q);
-  } else {
-    uint32_t w[16];
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const uint32_t x = col + j < vocab ? __bfloat16_as_ushort(bias[col + j]) : 0u;
-      w[j / 2] = j % 2 ? w[j / 2] | (x << 16) : x;
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) b.v[q] = make_uint4(w[q * 4], w[q * 4 + 1], w[q * 4 + 2], w[q * 4 + 3]);
-  }
+  for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
 }
-__device__ __forceinline__ void add_bias(const bf16* bias, const Bias32& b, float (&z)[32]) {
-  if (bias == nullptr) return;
+__device__ __forceinline__ void join_sum(float (&z)[32], uint32_t taddr) {
+  uint32_t v[32];
+  tmem_ld_32x32(taddr, v);
+  tmem_ld_wait();
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const uint32_t w[4] = {b.v[q].x, b.v[q].y, b.v[q].z, b.v[q].w};
+  for (int j = 0; j < 32; ++j) z[j] += __uint_as_float(v[j]);
+}
+// The same for blocks of 32 columns from taddr + begin on, `step` columns apart, those below `end`.
+template <int BLOCKS>
+__device__ __forceinline__ void join_sums(float (&z)[BLOCKS][32], uint32_t taddr, int begin, int step, int end) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      z[q * 8 + 2 * j] += bf16_lo(w[j]);
-      z[q * 8 + 2 * j + 1] += bf16_hi(w[j]);
+  for (int i = 0; i < BLOCKS; ++i) if (begin + i * step < end) join_sum(z[i], taddr + begin + i * step);   // (the same for the whole warp)
+}
+// The logits to where the last of their sums was, as if all terms had been summed there.
+template <int BLOCKS>
+__device__ __forceinline__ void put_sums(const float (&sum)[BLOCKS][32], uint32_t taddr, int begin, int step, int end) {
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i) {
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+      const int c = begin + i * step + h;
+      if (c >= end) continue;
+      uint32_t v[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(sum[i][h + j]);
+      tmem_st_32x16(taddr + c, v);
     }
+  }
+  tmem_st_wait();
+}
+
+// The bias of a thread's words, blocks of 32 from `col` on, `step` apart: all asked for before the first is used (block by block it took 700
+// clocks a block), and added to their logits.  At the vocabulary's end a lane reads that of one word per block, -inf behind the last word.
+template <int BLOCKS>
+__device__ __forceinline__ void add_bias(const bf16* bias, int col, int step, int vocab, int lane, float (&z)[BLOCKS][32]) {
+  if (col + (BLOCKS - 1) * step + 32 > vocab) {
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+      const int word = col + i * step + lane;
+      const float b = word >= vocab ? -INFINITY : (bias != nullptr ? __bfloat162float(bias[word]) : 0.f);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) z[i][j] += __shfl_sync(0xffffffffu, b, j);
+    }
+  } else if (bias != nullptr) {
+    uint4 v[BLOCKS][4];
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[i][q] = __ldg(reinterpret_cast<const uint4*>(bias + col + i * step) + q);
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t w[4] = {v[i][q].x, v[i][q].y, v[i][q].z, v[i][q].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          z[i][q * 8 + 2 * j] += bf16_lo(w[j]);
+          z[i][q * 8 + 2 * j + 1] += bf16_hi(w[j]);
+        }
+      }
   }
 }
 
@@ -244,10 +292,11 @@ __device__ __forceinline__ float column_sums(float (&c)[32], int lane) {
   return c[0];
 }
 
-template <bool GRAD>
-__global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
+template <Mode MODE>
+__global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
+  constexpr bool GRAD = MODE != kForward;
   constexpr int STAGES = kStages;
-  constexpr int EPILOGUE_WARPS = epilogue_warps(GRAD), GROUPS = groups(GRAD);
+  constexpr int EPILOGUE_WARPS = epilogue_warps(MODE), GROUPS = groups(MODE);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sA = smem_u32(smem);
@@ -306,19 +355,19 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
     }
   }
   // What the arguments alone decide is computed before the wait (a first look at each line of them costs some hundred clocks).
-  const bool given = GRAD ? p.work == nullptr : p.count == nullptr;
+  const bool given = MODE == kProducts || (MODE == kForward && p.count == nullptr);
   VocabWork work = {};
-  if (given) work = load_work<GRAD>(p);
+  if (given) work = load_work<MODE>(p);
   asm volatile("" ::"r"(p.rows), "r"(p.block_n), "r"(p.block_h), "r"(p.n_tiles), "r"(p.want_w), "l"(p.labels), "l"(p.counter));
   grid_dependency_wait();
   grid_launch_dependents();
-  if (!given) work = load_work<GRAD>(p);
+  if (!given) work = load_work<MODE>(p);
   const int rows = work.rows, g_pitch = p.piece << work.shift;
   const int gathered = rows == p.rows ? 0 : 1;      // which x: the caller's, or the rows with a label
   const int total = work.n0 + work.n1 + work.n2;
   const int k0 = (p.hidden + 63) / 64;
   const int first_term = (rows + 63) / 64;          // k-blocks of the first term of g in kind 2
-  const bool two_terms = GRAD && !p.by_words && p.want_w && terms_of_g(rows) == 2;
+  const bool two_terms = MODE == kGradient && p.want_w && terms_of_g(rows) == 2;
 
   // Tiles.  Forward: worker, worker + n_workers, ... (all tiles cost the same).  Backward: the first one likewise, then the next of the
   // list, whoever is free first; rank 0's producer takes them from a counter in memory and announces them to all roles of both CTAs.
@@ -355,340 +404,394 @@ __global__ void __launch_bounds__(threads(GRAD), 1) vocab_loss_pair_tcgen05(cons
     return t.kind >= 0;
   };
 
-  if (warp == 0) {
-    // ------------------------------ TMA producer ------------------------------
-    const bool leader = elect_one();
-    int stage = 0;
-    uint32_t phase = 0;
-    long long issued = 0;
-    bool ok = true;
-    // (backward, rank 0) The tile after the one whose copies are under way is asked for when its turn begins and announced some k-blocks
-    // later, so that neither the trip to the counter nor that to the other CTA holds up a copy.
-    int asked = 0;
-    if (GRAD && rank == 0 && lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
-    Tile ahead = t;
-    if (worker >= total) ahead.kind = -1;
-    auto announce = [&](int i) -> bool {
-      if (i < total) ahead = find_tile<GRAD>(work, p.n_tiles, k0, p.two_terms, i); else ahead.kind = -1;
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) return false;
-      if (lane < 2)
-        send_words(map_to_cta(smem_u32(const_cast<int4*>(slot_tile) + slot), lane), ahead.kind, ahead.m, ahead.n | (ahead.range << 16), ahead.k_blocks,
-                   map_to_cta(bar_slot_full + 8 * slot, lane));
-      __syncwarp();
-      if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
-      if (ahead.kind >= 0 && lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
-      return true;
-    };
-    for (bool first = true; ok; first = false) {
-      if (!GRAD) {
-        if (!next_static(first)) break;
-      } else if (rank != 0) {
-        if (!next_announced(first)) break;
-      } else {
-        t = ahead;
-        if (t.kind < 0) break;
-      }
-      const int half_n = (t.kind == 0 ? p.block_n : p.block_h) / 2;
-      const uint32_t bytes = 2 * (kStageA + half_n * 128);
-      const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf;
-      const int n0 = t.n * (2 * half_n) + static_cast<int>(rank) * half_n;
-      for (int kb = 0; kb < t.k_blocks; ++kb) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag))) { ok = false; break; }
-        if (leader) {
-          const uint32_t a = sA + stage * kStageA, b = sB + stage * kStageB, bar = bar_full_count + 8 * stage;
-          const int k = (t.k_begin + kb) * 64;
-          if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, bytes);
-          if (!GRAD || t.kind == 0) {
-            tma_load_2d_pair(a, &p.x_k[gathered], k, m0, bar);
-            tma_load_2d_pair(b, &p.w_k, k, work.col0 + n0, bar);
-          } else if (t.kind == 1) {
-            if (p.by_words) {
-              tma_load_2d_pair(a, &p.g_mn[work.shift], m0, work.prev_col0 + k, bar);
-              tma_load_2d_pair(a + 8192, &p.g_mn[work.shift], m0 + 64, work.prev_col0 + k, bar);
-            } else {
-              tma_load_2d_pair(a, &p.g_k[work.shift], k, work.prev_g_row0 + m0, bar);
-            }
-            tma_load_2d_pair(b, &p.w_mn, n0, work.prev_col0 + k, bar);
-            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, work.prev_col0 + k, bar);
-          } else {
-            if (p.by_words) {
-              tma_load_2d_pair(a, &p.g_k[work.shift], k, work.prev_col0 + m0, bar);
-            } else {
-              const int kg = work.prev_g_row0 + (kb < first_term ? k : k - first_term * 64 + kHalf);
-              tma_load_2d_pair(a, &p.g_mn[work.shift], m0, kg, bar);
-              tma_load_2d_pair(a + 8192, &p.g_mn[work.shift], m0 + 64, kg, bar);
-            }
-            const int kx = kb < first_term ? k : k - first_term * 64;   // (both terms meet the same rows of x)
-            tma_load_2d_pair(b, &p.x_mn[gathered], n0, kx, bar);
-            if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, kx, bar);
-          }
-        }
-        ++issued;
-        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        if (GRAD && rank == 0 && kb == min(3, t.k_blocks - 1) && !announce(n_workers + __shfl_sync(0xffffffffu, asked, 0))) { ok = false; break; }
-      }
-      if (GRAD && rank == 0 && ok && t.k_blocks == 0) ok = announce(n_workers + __shfl_sync(0xffffffffu, asked, 0));
-    }
-    if (!ok && rank == 0 && leader) {
-      // giving up: what is still in flight gets the same limit to land
-      const int pending = issued < STAGES ? static_cast<int>(issued) : STAGES;
-      for (int i = 0; i < pending; ++i) {
-        if (stage == 0) { stage = STAGES; phase ^= 1u; }
-        --stage;
-        mbar_drain(bar_full + 8 * stage, phase);
-      }
-    }
-  } else if (warp == 1) {
-    // ------------------------------ MMA issuer --------------------------------
-    const bool leader = elect_one();
-    if (rank == 0) {
-      int stage = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0;
+  if (warp < first_epilogue_warp(MODE)) {
+    if constexpr (MODE != kProducts) setmaxnreg_dec<kIssueRegs>();
+    if (warp == 0) {
+      // ------------------------------ TMA producer ------------------------------
+      const bool leader = elect_one();
+      int stage = 0;
+      uint32_t phase = 0;
+      long long issued = 0;
       bool ok = true;
+      // (backward, rank 0) The tile after the one whose copies are under way is asked for when its turn begins and announced some k-blocks
+      // later, so that neither the trip to the counter nor that to the other CTA holds up a copy.
+      int asked = 0;
+      if (GRAD && rank == 0 && lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
+      Tile ahead = t;
+      if (worker >= total) ahead.kind = -1;
+      auto announce = [&](int i) -> bool {
+        if (i < total) ahead = find_tile<GRAD>(work, p.n_tiles, k0, p.two_terms, i); else ahead.kind = -1;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_slot_empty + 8 * slot, slot_phase ^ 1u, abort_flag))) return false;
+        if (lane < 2)
+          send_words(map_to_cta(smem_u32(const_cast<int4*>(slot_tile) + slot), lane), ahead.kind, ahead.m, ahead.n | (ahead.range << 16), ahead.k_blocks,
+                     map_to_cta(bar_slot_full + 8 * slot, lane));
+        __syncwarp();
+        if (++slot == kSlots) { slot = 0; slot_phase ^= 1u; }
+        if (ahead.kind >= 0 && lane == 0) asked = static_cast<int>(atomicAdd(p.counter, 1u));
+        return true;
+      };
       for (bool first = true; ok; first = false) {
-        if (GRAD ? !next_announced(first) : !next_static(first)) break;
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) break;
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kTile);
-        const bool mn_a = GRAD && t.kind == (p.by_words ? 1 : 2), mn_b = GRAD && t.kind != 0;
-        const uint32_t idesc = umma_idesc_bf16(kTile, t.kind == 0 ? p.block_n : p.block_h) | (mn_a ? kAlongMnA : 0u) | (mn_b ? kAlongMnB : 0u);
-        // 16 elements of K on: 32 bytes inside a row, or 16 rows
-        const uint64_t step_a = mn_a ? 2048 >> 4 : 2, step_b = mn_b ? 2048 >> 4 : 2;
-        for (int kb = 0; kb < t.k_blocks; ++kb) {
-          if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
-          tc_fence_after();
-          if (leader) {
-            const uint64_t da = mn_a ? smem_desc_mn(sA + stage * kStageA) : smem_desc_sw128(sA + stage * kStageA);
-            const uint64_t db = mn_b ? smem_desc_mn(sB + stage * kStageB) : smem_desc_sw128(sB + stage * kStageB);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16_pair(d_tmem, da + step_a * k, db + step_b * k, idesc, (kb | k) != 0 ? 1u : 0u);
-            umma_commit_pair(bar_empty + 8 * stage);
-          }
-          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        if (!GRAD) {
+          if (!next_static(first)) break;
+        } else if (rank != 0) {
+          if (!next_announced(first)) break;
+        } else {
+          t = ahead;
+          if (t.kind < 0) break;
         }
-        if (!ok) break;
-        if (leader) umma_commit_pair(bar_acc_full + 8 * acc);
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        const int half_n = (t.kind == 0 ? p.block_n : p.block_h) / 2;
+        const uint32_t bytes = 2 * (kStageA + half_n * 128);
+        const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf;
+        const int n0 = t.n * (2 * half_n) + static_cast<int>(rank) * half_n;
+        for (int kb = 0; kb < t.k_blocks; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag))) { ok = false; break; }
+          if (leader) {
+            const uint32_t a = sA + stage * kStageA, b = sB + stage * kStageB, bar = bar_full_count + 8 * stage;
+            const int k = (t.k_begin + kb) * 64;
+            if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, bytes);
+            if (MODE == kForward || (MODE == kGradient && t.kind == 0)) {
+              tma_load_2d_pair(a, &p.x_k[gathered], k, m0, bar);
+              tma_load_2d_pair(b, &p.w_k, k, work.col0 + n0, bar);
+            } else if (t.kind == 1) {
+              if (MODE == kProducts) {
+                tma_load_2d_pair(a, &p.g_mn[work.shift], m0, work.prev_col0 + k, bar);
+                tma_load_2d_pair(a + 8192, &p.g_mn[work.shift], m0 + 64, work.prev_col0 + k, bar);
+              } else {
+                tma_load_2d_pair(a, &p.g_k[work.shift], k, work.prev_g_row0 + m0, bar);
+              }
+              tma_load_2d_pair(b, &p.w_mn, n0, work.prev_col0 + k, bar);
+              if (half_n > 64) tma_load_2d_pair(b + 8192, &p.w_mn, n0 + 64, work.prev_col0 + k, bar);
+            } else {
+              if (MODE == kProducts) {
+                tma_load_2d_pair(a, &p.g_k[work.shift], k, work.prev_col0 + m0, bar);
+              } else {
+                const int kg = work.prev_g_row0 + (kb < first_term ? k : k - first_term * 64 + kHalf);
+                tma_load_2d_pair(a, &p.g_mn[work.shift], m0, kg, bar);
+                tma_load_2d_pair(a + 8192, &p.g_mn[work.shift], m0 + 64, kg, bar);
+              }
+              const int kx = kb < first_term ? k : k - first_term * 64;   // (both terms meet the same rows of x)
+              tma_load_2d_pair(b, &p.x_mn[gathered], n0, kx, bar);
+              if (half_n > 64) tma_load_2d_pair(b + 8192, &p.x_mn[gathered], n0 + 64, kx, bar);
+            }
+          }
+          ++issued;
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          if (GRAD && rank == 0 && kb == min(3, t.k_blocks - 1) && !announce(n_workers + __shfl_sync(0xffffffffu, asked, 0))) { ok = false; break; }
+        }
+        if (GRAD && rank == 0 && ok && t.k_blocks == 0) ok = announce(n_workers + __shfl_sync(0xffffffffu, asked, 0));
+      }
+      if (!ok && rank == 0 && leader) {
+        // giving up: what is still in flight gets the same limit to land
+        const int pending = issued < STAGES ? static_cast<int>(issued) : STAGES;
+        for (int i = 0; i < pending; ++i) {
+          if (stage == 0) { stage = STAGES; phase ^= 1u; }
+          --stage;
+          mbar_drain(bar_full + 8 * stage, phase);
+        }
+      }
+    } else if (warp == 1) {
+      // ------------------------------ MMA issuer --------------------------------
+      const bool leader = elect_one();
+      if (rank == 0) {
+        int stage = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        bool ok = true;
+        for (bool first = true; ok; first = false) {
+          if (GRAD ? !next_announced(first) : !next_static(first)) break;
+          const bool mn_a = GRAD && t.kind == (MODE == kProducts ? 1 : 2), mn_b = GRAD && t.kind != 0;
+          const uint32_t idesc = umma_idesc_bf16(kTile, t.kind == 0 ? p.block_n : p.block_h) | (mn_a ? kAlongMnA : 0u) | (mn_b ? kAlongMnB : 0u);
+          // 16 elements of K on: 32 bytes inside a row, or 16 rows
+          const uint64_t step_a = mn_a ? 2048 >> 4 : 2, step_b = mn_b ? 2048 >> 4 : 2;
+          const int most = MODE != kProducts && t.kind == 0 ? sum_blocks(GRAD, k0) : max(t.k_blocks, 1);
+          int kb = 0;
+          do {                                            // (once where there is nothing to sum)
+            if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kTile);
+            const int begin = kb, end = min(kb + most, t.k_blocks);
+            for (; kb < end; ++kb) {
+              if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
+              tc_fence_after();
+              if (leader) {
+                const uint64_t da = mn_a ? smem_desc_mn(sA + stage * kStageA) : smem_desc_sw128(sA + stage * kStageA);
+                const uint64_t db = mn_b ? smem_desc_mn(sB + stage * kStageB) : smem_desc_sw128(sB + stage * kStageB);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) umma_bf16_pair(d_tmem, da + step_a * k, db + step_b * k, idesc, (kb - begin) | k ? 1u : 0u);
+                umma_commit_pair(bar_empty + 8 * stage);
+              }
+              if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+            if (!ok) break;
+            if (leader) umma_commit_pair(bar_acc_full + 8 * acc);
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+          } while (kb < t.k_blocks);
+        }
       }
     }
   } else {
     // ------------------------------ epilogue ----------------------------------
-    const int e = warp - 2;
+    if constexpr (MODE != kProducts) setmaxnreg_inc<kEpilogueRegs>();
+    const int e = warp - first_epilogue_warp(MODE);
     const int quarter = warp & 3;
     const int group = e >> 2;
     const uint32_t bar_acc_empty_0 = map_to_cta(bar_acc_empty, 0);
+    const int sums = (k0 + sum_blocks(GRAD, k0) - 1) / sum_blocks(GRAD, k0);
     int acc = 0;
     uint32_t acc_phase = 0;
-    for (bool first = true;; first = false) {
-      if (GRAD ? !next_announced(first) : !next_static(first)) break;
-      const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32;   // of this warp
-      const int row = m0 + lane;
-      const bool row_counts = row < rows;
-      int label = -1;
-      float4 shift = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (t.kind == 0 && row_counts) {
-        label = p.labels[row];
-        if (GRAD) {
-          shift = p.row_shift[row];
-        }
-      }
-      if (t.kind == 0 && p.bias != nullptr && lane < 4) {   // the tile's bias, a line per 64 columns, on its way while the tile is computed
-        const int col = work.col0 + t.n * p.block_n + lane * 64;
-        if (col < p.vocab) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.bias + col));
-      }
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * acc, acc_phase, abort_flag))) break;
-      tc_fence_after();
-      const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc * kTile);
-      if (!GRAD) {
-        float top = kFloor, sum = 0.f;                  // largest logit, sum of exp(z - top)
-        const int n0 = t.n * p.block_n;
-#pragma unroll 1
-        for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
-          const int col = n0 + c;
-          if (col >= p.vocab || m0 >= rows) break;
-          Bias32 bias;
-          load_bias(p.bias, col, p.vocab, bias);
-          uint32_t v[32];
-          tmem_ld_32x32(taddr0 + c, v);
-          tmem_ld_wait();
-          float z[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = with_cut_off(v[j], p.cut_off);
-          add_bias(p.bias, bias, z);
-          if (col + 32 > p.vocab) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) if (col + j >= p.vocab) z[j] = -INFINITY;
-          }
-          const int at = label - col;
-          if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
-            float mine = 0.f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) if (j == at) mine = z[j];
-            if (at >= 0 && at < 32) p.label_logit[row] = mine;
-          }
-          float m = z[0];
-#pragma unroll
-          for (int j = 1; j < 32; ++j) m = fmaxf(m, z[j]);
-          const float next = fmaxf(top, m);
-          sum *= ex2_approx((top - next) * kLog2e);
-          top = next;
-          float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < 32; ++j) s[j & 3] += ex2_approx((z[j] - top) * kLog2e);   // (differences first: logits may be at the lowest number)
-          sum += (s[0] + s[1]) + (s[2] + s[3]);
-        }
-        if (row_counts) p.parts[static_cast<int64_t>(row) * p.part_pitch + GROUPS * t.n + group] = make_float2(top, sum);
-      } else if (t.kind == 0) {
-        const int n0 = t.n * p.block_n;                 // in the piece
-        const bool whole = __all_sync(0xffffffffu, row_counts);
-        bf16* g_out = p.g + static_cast<int64_t>(work.g_row0 + m0 + (lane & ~3)) * g_pitch + (lane & 3) * 8;
-#pragma unroll 1
-        for (int c = group * 32; c < p.block_n; c += 32 * GROUPS) {
-          const int local = n0 + c;
-          // (in whole k-blocks of the products that sum over columns and over rows)
-          if (local >= (work.cols + 63) / 64 * 64 || m0 >= (rows + 63) / 64 * 64) break;
-          const int col = work.col0 + local;
-          Bias32 bias;
-          load_bias(p.bias, col, p.vocab, bias);
-          uint32_t v[32];
-          tmem_ld_32x32(taddr0 + c, v);
-          tmem_ld_wait();
-          float g[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] = with_cut_off(v[j], p.cut_off);
-          add_bias(p.bias, bias, g);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j] - shift.x, kLog2e, shift.y));
-          if (__any_sync(0xffffffffu, shift.z < 0.f)) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] = shift.z < 0.f ? -g[j] : g[j];
-          }
-          const int at = label - col;
-          const bool hit = __any_sync(0xffffffffu, at >= 0 && at < 32);
-          if (hit) {
-            float mine = 0.f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              if (j == at) {
-                g[j] -= shift.z;
-                mine = g[j];
-              }
-            }
-            // what rounding takes from the label's entry
-            if (at >= 0 && at < 32) p.row_residual[row] = mine - __bfloat162float(__float2bfloat16_rn(mine));
-          }
-          if (!whole) {                                 // (behind the last row lies anything)
-#pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] = row_counts ? g[j] : 0.f;
-          }
-          if (col + 32 > p.vocab) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] = col + j < p.vocab ? g[j] : 0.f;
-          }
-          uint4 out[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            out[q] = make_uint4(pack_bf16(g[q * 8], g[q * 8 + 1]), pack_bf16(g[q * 8 + 2], g[q * 8 + 3]), pack_bf16(g[q * 8 + 4], g[q * 8 + 5]),
-                                pack_bf16(g[q * 8 + 6], g[q * 8 + 7]));
-          exchange_pieces(out, lane);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(q) * g_pitch + local) = out[q];
-          if (two_terms) {
-            auto rest = [&](int j) { return g[j] - __bfloat162float(__float2bfloat16_rn(g[j])); };
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              out[q] = make_uint4(pack_bf16(rest(q * 8), rest(q * 8 + 1)), pack_bf16(rest(q * 8 + 2), rest(q * 8 + 3)),
-                                  pack_bf16(rest(q * 8 + 4), rest(q * 8 + 5)), pack_bf16(rest(q * 8 + 6), rest(q * 8 + 7)));
-            exchange_pieces(out, lane);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(kHalf + q) * g_pitch + local) = out[q];
-          }
-          if (p.bias_parts != nullptr && m0 < rows) {
-            const float s = column_sums(g, lane);
-            if (local + lane < work.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + col + lane] = s;
-          }
-        }
-      } else if (t.kind == 1) {
-        const int n0 = t.n * p.block_h;
-        float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * work.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
-#pragma unroll 1
-        for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
-          if (n0 + c >= p.hidden || m0 >= rows) break;
-          uint32_t v[32];
-          if (t.k_blocks > 0) {
-            tmem_ld_32x32(taddr0 + c, v);
-            tmem_ld_wait();
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0u;
-          }
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint4 out[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              out[q] = make_uint4(v[half * 16 + q * 4], v[half * 16 + q * 4 + 1], v[half * 16 + q * 4 + 2], v[half * 16 + q * 4 + 3]);
-            exchange_pieces(out, lane);
-            const int col = n0 + c + half * 16;
-            if (col + (lane & 3) * 4 >= p.hidden) continue;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float* to = sums + static_cast<int64_t>(q) * p.hidden + col;
-              if (work.prev_col0 == 0) *reinterpret_cast<uint4*>(to) = out[q]; else red_add_v4(to, out[q]);
-            }
-          }
-        }
-      } else {
-        const int n0 = t.n * p.block_h;
-        const int word = work.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
-        bf16* dw = p.dw + static_cast<int64_t>(word) * p.dw_stride + (lane & 3) * 8;
-#pragma unroll 1
-        for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
-          const int col = n0 + c;
-          if (col >= p.hidden || work.prev_col0 + m0 >= p.vocab) break;
-          uint32_t v[32];
-          if (t.k_blocks > 0) {
-            tmem_ld_32x32(taddr0 + c, v);
-            tmem_ld_wait();
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0u;
-          }
-          if (p.accumulate) {
-            const int mine = work.prev_col0 + row;
-            const bf16* old = p.dw + static_cast<int64_t>(mine) * p.dw_stride + col;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {               // (hidden is a multiple of eight)
-              if (mine >= p.vocab || col + q * 8 >= p.hidden) continue;
-              const uint4 b = *reinterpret_cast<const uint4*>(old + q * 8);
-              const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                v[q * 8 + 2 * j] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j]) + bf16_lo(w[j]));
-                v[q * 8 + 2 * j + 1] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j + 1]) + bf16_hi(w[j]));
-              }
-            }
-            __syncwarp();                               // (all of the warp has read before any of it writes)
-          }
-          uint4 out[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t o[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = pack_bf16(__uint_as_float(v[q * 8 + 2 * j]), __uint_as_float(v[q * 8 + 2 * j + 1]));
-            out[q] = make_uint4(o[0], o[1], o[2], o[3]);
-          }
-          exchange_pieces(out, lane);
-          if (col + (lane & 3) * 8 >= p.hidden) continue;
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (word + q < p.vocab) *reinterpret_cast<uint4*>(dw + static_cast<int64_t>(q) * p.dw_stride + col) = out[q];
-        }
-      }
+    const uint32_t my_tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+    auto wait_sum = [&] { return __all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * acc, acc_phase, abort_flag)); };
+    auto leave_sum = [&] {
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_remote(bar_acc_empty_0 + 8 * acc);
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    };
+    if constexpr (MODE == kForward) {
+      constexpr int BLOCKS = kTile / 32 / GROUPS;
+      float z[BLOCKS][32];
+      bool taken = false;                               // the first sum of the tile's logits is there already
+      auto take = [&](int i, int end) {
+        const int c = group * 32 + 32 * GROUPS * i;
+        if (c < end) take_sum(z[i], my_tmem + static_cast<uint32_t>(acc * kTile + c));
+      };
+      // A tile's labels, and its bias on the way to L1, while the tile before is worked on.
+      int next_label = -1;
+      auto next_tile = [&](bool first) -> bool {
+        if (!next_static(first)) return false;
+        const int row = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 + lane, col = t.n * p.block_n + lane * 16;
+        next_label = row < rows ? p.labels[row] : -1;
+        if (p.bias != nullptr && lane < 16 && col < p.vocab)
+          asm volatile("{\n\t.reg .b16 t;\n\tld.global.nc.b16 t, [%0];\n\t}" ::"l"(p.bias + col));
+        return true;
+      };
+      for (bool more = next_tile(true); more;) {
+        const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32;   // of this warp
+        const int row = m0 + lane, n0 = t.n * p.block_n;
+        const int end = m0 < rows ? min(p.block_n, p.vocab - n0) : 0;
+        const int label = next_label;
+        float2* part = p.parts + static_cast<int64_t>(row) * p.part_pitch + GROUPS * t.n + group;
+        if (!taken) {
+          if (!wait_sum()) break;
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < BLOCKS; ++i) take(i, end);
+          leave_sum();
+        }
+        add_bias(p.bias, n0 + group * 32, 32 * GROUPS, p.vocab, lane, z);
+        bool ok = true;
+        for (int i = 1; i < sums; ++i) {
+          if (!(ok = wait_sum())) break;
+          tc_fence_after();
+          join_sums(z, my_tmem + static_cast<uint32_t>(acc * kTile), group * 32, 32 * GROUPS, end);
+          leave_sum();
+        }
+        if (!ok) break;
+        if (__any_sync(0xffffffffu, label >= n0 && label < n0 + end)) {
+          float mine = 0.f;
+          bool here = false;
+#pragma unroll
+          for (int i = 0; i < BLOCKS; ++i) {
+            const int at = label - (n0 + group * 32 + 32 * GROUPS * i);
+            here |= at >= 0 && at < 32 && label < n0 + end;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) if (j == at) mine = z[i][j];
+          }
+          if (here) p.label_logit[row] = mine;
+        }
+        float top = kFloor, s[4] = {0.f, 0.f, 0.f, 0.f};   // largest logit, sum of exp(z - top)
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+          if (group * 32 + 32 * GROUPS * i >= end) continue;
+          float m[4] = {z[i][0], z[i][1], z[i][2], z[i][3]};
+#pragma unroll
+          for (int j = 4; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], z[i][j]);
+          top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+        }
+        // The exponentials keep the special-function units busy for 2048 clocks.  Half way through, the first sum of the next tile is there and
+        // takes the place of the logits that are done with: otherwise the MMAs, which are two sums ahead, would wait for it.
+        more = next_tile(false);
+        taken = more && sums > 1;
+        const int next_end = taken && t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 < rows ? min(p.block_n, p.vocab - t.n * p.block_n) : 0;
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+          if (group * 32 + 32 * GROUPS * i < end) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[j & 3] += ex2_approx((z[i][j] - top) * kLog2e);   // (differences first: logits may be at the lowest number)
+          }
+          if (i == BLOCKS / 2) {
+            if (taken && !(ok = wait_sum())) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < i; ++k) take(k, next_end);
+          }
+          if (i >= BLOCKS / 2) take(i, next_end);
+        }
+        if (!ok) break;
+        if (taken) leave_sum();
+        if (row < rows) *part = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+      }
+    } else {
+      for (bool first = true; next_announced(first); first = false) {
+        const int m0 = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32;   // of this warp
+        const int row = m0 + lane;
+        const bool row_counts = row < rows;
+        if (MODE != kProducts && t.kind == 0) {
+          const int label = row_counts ? p.labels[row] : -1;
+          const float4 shift = row_counts ? p.row_shift[row] : make_float4(0.f, 0.f, 0.f, 0.f);
+          // The logits of this warp's rows and columns, in registers: the last of their accumulators is free before anything is done with them.
+          const int n0 = t.n * p.block_n;                 // in the piece
+          // (what anything below looks at: in whole k-blocks of the products that sum over columns and over rows)
+          const int columns = m0 >= (rows + 63) / 64 * 64 ? 0 : min(p.block_n, (work.cols - n0 + 63) / 64 * 64);
+          float z[kTile / 32 / GROUPS][32] = {};
+          add_bias(p.bias, work.col0 + n0 + group * 32, 32 * GROUPS, p.vocab, lane, z);
+          bool ok = true;
+          for (int i = 0; ok && i < sums; ++i) {
+            if (!(ok = wait_sum())) break;
+            tc_fence_after();
+            join_sums(z, my_tmem + static_cast<uint32_t>(acc * kTile), group * 32, 32 * GROUPS, columns);
+            leave_sum();
+          }
+          if (!ok) break;
+          const bool whole = __all_sync(0xffffffffu, row_counts);
+          bf16* g_out = p.g + static_cast<int64_t>(work.g_row0 + m0 + (lane & ~3)) * g_pitch + (lane & 3) * 8;
+#pragma unroll
+          for (int i = 0; i < kTile / 32 / GROUPS; ++i) {
+            const int c = group * 32 + 32 * GROUPS * i;
+            if (c >= columns) break;
+            const int local = n0 + c;
+            const int col = work.col0 + local;
+            float (&g)[32] = z[i];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j] - shift.x, kLog2e, shift.y));
+            if (__any_sync(0xffffffffu, shift.z < 0.f)) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) g[j] = shift.z < 0.f ? -g[j] : g[j];
+            }
+            const int at = label - col;
+            const bool hit = __any_sync(0xffffffffu, at >= 0 && at < 32);
+            if (hit) {
+              float mine = 0.f;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                if (j == at) {
+                  g[j] -= shift.z;
+                  mine = g[j];
+                }
+              }
+              // what rounding takes from the label's entry
+              if (at >= 0 && at < 32) p.row_residual[row] = mine - __bfloat162float(__float2bfloat16_rn(mine));
+            }
+            if (!whole) {                               // (behind the last row lies anything)
+#pragma unroll
+              for (int j = 0; j < 32; ++j) g[j] = row_counts ? g[j] : 0.f;
+            }
+            uint4 out[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              out[q] = make_uint4(pack_bf16(g[q * 8], g[q * 8 + 1]), pack_bf16(g[q * 8 + 2], g[q * 8 + 3]), pack_bf16(g[q * 8 + 4], g[q * 8 + 5]),
+                                  pack_bf16(g[q * 8 + 6], g[q * 8 + 7]));
+            exchange_pieces(out, lane);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(q) * g_pitch + local) = out[q];
+            if (two_terms) {
+              auto rest = [&](int j) { return g[j] - __bfloat162float(__float2bfloat16_rn(g[j])); };
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                out[q] = make_uint4(pack_bf16(rest(q * 8), rest(q * 8 + 1)), pack_bf16(rest(q * 8 + 2), rest(q * 8 + 3)),
+                                    pack_bf16(rest(q * 8 + 4), rest(q * 8 + 5)), pack_bf16(rest(q * 8 + 6), rest(q * 8 + 7)));
+              exchange_pieces(out, lane);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(g_out + static_cast<int64_t>(kHalf + q) * g_pitch + local) = out[q];
+            }
+            if (p.bias_parts != nullptr && m0 < rows) {
+              const float s = column_sums(g, lane);
+              if (local + lane < work.cols) p.bias_parts[static_cast<int64_t>(m0 / 32) * p.bias_pitch + col + lane] = s;
+            }
+          }
+          continue;
+        }
+        if (!wait_sum()) break;
+        tc_fence_after();
+        const uint32_t taddr0 = my_tmem + static_cast<uint32_t>(acc * kTile);
+        if (t.kind == 1) {
+          const int n0 = t.n * p.block_h;
+          float* sums = p.dx_sums + (static_cast<int64_t>(t.range) * work.row_pitch + m0 + (lane & ~3)) * p.hidden + (lane & 3) * 4;
+#pragma unroll 1
+          for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
+            if (n0 + c >= p.hidden || m0 >= rows) break;
+            uint32_t v[32];
+            if (t.k_blocks > 0) {
+              tmem_ld_32x32(taddr0 + c, v);
+              tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = 0u;
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint4 out[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                out[q] = make_uint4(v[half * 16 + q * 4], v[half * 16 + q * 4 + 1], v[half * 16 + q * 4 + 2], v[half * 16 + q * 4 + 3]);
+              exchange_pieces(out, lane);
+              const int col = n0 + c + half * 16;
+              if (col + (lane & 3) * 4 >= p.hidden) continue;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                float* to = sums + static_cast<int64_t>(q) * p.hidden + col;
+                if (work.prev_col0 == 0) *reinterpret_cast<uint4*>(to) = out[q]; else red_add_v4(to, out[q]);
+              }
+            }
+          }
+        } else {
+          const int n0 = t.n * p.block_h;
+          const int word = work.prev_col0 + m0 + (lane & ~3);   // row of dW of this lane's first piece
+          bf16* dw = p.dw + static_cast<int64_t>(word) * p.dw_stride + (lane & 3) * 8;
+#pragma unroll 1
+          for (int c = group * 32; c < p.block_h; c += 32 * GROUPS) {
+            const int col = n0 + c;
+            if (col >= p.hidden || work.prev_col0 + m0 >= p.vocab) break;
+            uint32_t v[32];
+            if (t.k_blocks > 0) {
+              tmem_ld_32x32(taddr0 + c, v);
+              tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = 0u;
+            }
+            if (p.accumulate) {
+              const int mine = work.prev_col0 + row;
+              const bf16* old = p.dw + static_cast<int64_t>(mine) * p.dw_stride + col;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {               // (hidden is a multiple of eight)
+                if (mine >= p.vocab || col + q * 8 >= p.hidden) continue;
+                const uint4 b = *reinterpret_cast<const uint4*>(old + q * 8);
+                const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  v[q * 8 + 2 * j] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j]) + bf16_lo(w[j]));
+                  v[q * 8 + 2 * j + 1] = __float_as_uint(__uint_as_float(v[q * 8 + 2 * j + 1]) + bf16_hi(w[j]));
+                }
+              }
+              __syncwarp();                               // (all of the warp has read before any of it writes)
+            }
+            uint4 out[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              uint32_t o[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[j] = pack_bf16(__uint_as_float(v[q * 8 + 2 * j]), __uint_as_float(v[q * 8 + 2 * j + 1]));
+              out[q] = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+            exchange_pieces(out, lane);
+            if (col + (lane & 3) * 8 >= p.hidden) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (word + q < p.vocab) *reinterpret_cast<uint4*>(dw + static_cast<int64_t>(q) * p.dw_stride + col) = out[q];
+          }
+        }
+        leave_sum();
+      }
     }
   }
 
@@ -716,6 +819,7 @@ __device__ __forceinline__ float4 weighted_shift(float lse, float weight) { retu
 // word and all rows.
 //   forward   largest logit and sum of exponentials of a row over the 32 words of a warp: halves of the rows are exchanged for halves of the
 //             words (as column_sums), running over the CTA's tiles; the four warps are put together at the end
+//   Logits wider than four k-blocks are made in sums (see sum_blocks) that go through registers back to the last one's accumulator.
 //   backward  g by words, [vocab][64 or 128 rows], zeros in rows without a label and behind the last: as it is the operand along K for dW and
 //             the MN-major one for dx; db is a thread's own sum.  A row of dW whose word is a label is little else than that entry of g
 //             times a row of x, and with so few rows such entries are most of dW: where one of 256 words is a label, g of all of them is
@@ -728,7 +832,8 @@ constexpr int kFewMaxStages = 12;
 constexpr int kFewStageA = 128 * 128;
 constexpr int kFewBook = 8192;
 constexpr int kFewRing = 227 * 1024 - 1024 - kFewBook;
-constexpr uint32_t kFewTmemCols = 256;
+constexpr int kFewAccs = 4;              // accumulators, of a sum of a tile's logits each
+constexpr uint32_t kFewTmemCols = kFewAccs * kFewRows;
 
 // Largest over the 32 lanes of a warp of 32 columns each, column `lane` in the result (see column_sums).
 __device__ __forceinline__ float column_max(const float (&z)[32], int lane) {
@@ -760,19 +865,22 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
   const uint32_t bar_full = smem_u32(book);
   const uint32_t bar_empty = bar_full + 8 * kFewMaxStages;
   const uint32_t bar_acc_full = bar_empty + 8 * kFewMaxStages;
-  const uint32_t bar_acc_empty = bar_acc_full + 16;
-  const uint32_t bar_db = bar_acc_empty + 16;           // (backward) [accumulator][quarter]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * kFewMaxStages + 4 + 8));
+  const uint32_t bar_acc_empty = bar_acc_full + 8 * kFewAccs;
+  const uint32_t bar_db = bar_acc_empty + 8 * kFewAccs;  // (backward) [accumulator][quarter]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * kFewMaxStages + 6 * kFewAccs));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_label = reinterpret_cast<int*>(book + 512);                    // of every row; -1 where it takes no part
   float4* s_row = reinterpret_cast<float4*>(book + 512 + 512);          // (backward) weighted_shift
   float2* s_part = reinterpret_cast<float2*>(book + 512 + 512 + 2048);  // (forward) [quarter][row]
   float* s_db = reinterpret_cast<float*>(s_part);                       // (backward) [accumulator][quarter][word]
-  static_assert(8 * (2 * kFewMaxStages + 12) + 8 <= 512 && 512 + 512 + 2048 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
+  static_assert(8 * (2 * kFewMaxStages + 6 * kFewAccs) + 8 <= 512 && 512 + 512 + 2048 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
+  static_assert(kFewAccs * 4 * 32 * 4 <= 4 * kFewRows * 8, "sums of db");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int stages = p.stages, stage_bytes = p.stage_bytes;
   const int k_blocks = (p.hidden + 63) / 64;
+  constexpr int SUM_BLOCKS = 4 / STAGE_BLOCKS * STAGE_BLOCKS;   // k-blocks of a sum, in whole stages
+  const int sums = (k_blocks + SUM_BLOCKS - 1) / SUM_BLOCKS;
   constexpr uint32_t STAGE_A = STAGE_BLOCKS * kFewStageA;
   const int tiles = (p.vocab + 127) / 128;
   if (tid == 0) {
@@ -780,11 +888,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
       mbar_init(bar_full + 8 * s, 1);
       mbar_init(bar_empty + 8 * s, 1);
     }
-    for (int a = 0; a < 2; ++a) {
+    for (int a = 0; a < kFewAccs; ++a) {
       mbar_init(bar_acc_full + 8 * a, 1);
       mbar_init(bar_acc_empty + 8 * a, kFewWarps);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(bar_db + 8 * i, 1);
+    for (int i = 0; i < 4 * kFewAccs; ++i) mbar_init(bar_db + 8 * i, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -840,27 +948,30 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
     uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
     for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) break;
-      tc_fence_after();
-      const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kFewRows);
-      for (int kb = 0; kb < k_blocks; kb += STAGE_BLOCKS) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
+      for (int begin = 0; begin < k_blocks && ok; begin += SUM_BLOCKS) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag))) { ok = false; break; }
         tc_fence_after();
-        if (leader) {
+        const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kFewRows);
+        const int end = min(begin + SUM_BLOCKS, k_blocks);
+        for (int kb = begin; kb < end; kb += STAGE_BLOCKS) {
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
+          tc_fence_after();
+          if (leader) {
 #pragma unroll
-          for (int j = 0; j < STAGE_BLOCKS; ++j) {
-            const uint64_t da = smem_desc_sw128(ring + stage * stage_bytes + j * kFewStageA);
-            const uint64_t db = smem_desc_sw128(ring + stage * stage_bytes + STAGE_A + j * p.columns * 128);
+            for (int j = 0; j < STAGE_BLOCKS; ++j) {
+              const uint64_t da = smem_desc_sw128(ring + stage * stage_bytes + j * kFewStageA);
+              const uint64_t db = smem_desc_sw128(ring + stage * stage_bytes + STAGE_A + j * p.columns * 128);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(d_tmem, da + 2 * k, db + 2 * k, idesc, (kb | j | k) != 0 ? 1u : 0u);
+              for (int k = 0; k < 4; ++k) umma_bf16(d_tmem, da + 2 * k, db + 2 * k, idesc, (kb - begin) | j | k ? 1u : 0u);
+            }
+            umma_commit(bar_empty + 8 * stage);
           }
-          umma_commit(bar_empty + 8 * stage);
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
-        if (++stage == stages) { stage = 0; phase ^= 1u; }
+        if (!ok) break;
+        if (leader) umma_commit(bar_acc_full + 8 * acc);
+        if (++acc == kFewAccs) { acc = 0; acc_phase ^= 1u; }
       }
-      if (!ok) break;
-      if (leader) umma_commit(bar_acc_full + 8 * acc);
-      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
   } else {
     // ------------------------------ epilogue ----------------------------------
@@ -893,14 +1004,37 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
       for (int i = half; i < 4; i += 2) my_part[i * 32] = make_float2(kFloor, 0.f);
     }
     int acc = 0;
-    uint32_t acc_phase = 0;
+    uint32_t acc_phase = 0, db_phases = 0;                          // (a bit per accumulator)
+    auto wait_sum = [&] { return __all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * acc, acc_phase, abort_flag)); };
+    auto leave_sum = [&] {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_acc_empty + 8 * acc);
+      if (++acc == kFewAccs) { acc = 0; acc_phase ^= 1u; }
+    };
+    const int chunks = ((GRAD ? p.g_pitch : p.rows) + 31) / 32;
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
       const int word0 = tile * 128 + quarter * 32, word = word0 + lane;
       const bool is_word = word < p.vocab;
       const float bias = p.bias != nullptr && is_word ? __bfloat162float(p.bias[word]) : 0.f;
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * acc, acc_phase, abort_flag))) break;
-      tc_fence_after();
-      const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc * kFewRows);
+      const uint32_t my_tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+      if (sums > 1) {
+        float sum[kFewRows / 64][32] = {};
+        bool ok = true;
+        for (int i = 0;; ++i) {
+          if (!(ok = wait_sum())) break;
+          tc_fence_after();
+          join_sums(sum, my_tmem + static_cast<uint32_t>(acc * kFewRows), half * 32, 64, chunks * 32);
+          if (i + 1 == sums) break;
+          leave_sum();
+        }
+        if (!ok) break;
+        put_sums(sum, my_tmem + static_cast<uint32_t>(acc * kFewRows), half * 32, 64, chunks * 32);
+      } else {
+        if (!wait_sum()) break;
+        tc_fence_after();
+      }
+      const uint32_t taddr0 = my_tmem + static_cast<uint32_t>(acc * kFewRows);
       float db = 0.f;
       bool two_terms = false;                                       // one of the 256 words that a tile of dW has is a label
       if (GRAD) {
@@ -913,7 +1047,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
         two_terms = __any_sync(0xffffffffu, mine);
         if ((tile & 1) == 0 && quarter == 0 && half == 0 && lane == 0) p.two_terms[tile >> 1] = two_terms ? 1 : 0;
       }
-      const int chunks = ((GRAD ? p.g_pitch : p.rows) + 31) / 32;
       // (not unrolled: four copies of the body are more than the instruction cache holds; the first tile took 13 k clocks with them)
 #pragma unroll 1
       for (int i = half; i < chunks; i += 2) {
@@ -922,7 +1055,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
         tmem_ld_wait();
         float z[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) z[j] = with_cut_off(v[j], p.cut_off) + bias;
+        for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]) + bias;
         const int my_label = s_label[i * 32 + lane];                // of row i * 32 + lane
         // rows whose label is one of this warp's words
         uint32_t hits = __ballot_sync(0xffffffffu, my_label >= word0 && my_label < word0 + 32);
@@ -1001,15 +1134,13 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
           __syncwarp();
           if (lane == 0) mbar_arrive(bar);
         } else {
-          if (!__all_sync(0xffffffffu, mbar_wait(bar, acc_phase, abort_flag))) break;
+          if (!__all_sync(0xffffffffu, mbar_wait(bar, (db_phases >> acc) & 1u, abort_flag))) break;
           db += *other;
         }
+        db_phases ^= 1u << acc;
       }
       if (GRAD && p.db != nullptr && half == 0 && is_word) p.db[word] = p.accumulate ? p.db[word] + db : db;
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_acc_empty + 8 * acc);
-      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      leave_sum();
     }
   }
 
@@ -1348,9 +1479,9 @@ cudaError_t launch_few(const VocabFewParams& p, int sm_count, int* ctas, cudaStr
   }
 }
 
-template <bool GRAD>
+template <Mode MODE>
 cudaError_t launch_pairs(const VocabLossParams& p, int tiles, int sm_count, cudaStream_t stream) {
-  auto kernel = vocab_loss_pair_tcgen05<GRAD>;
+  auto kernel = vocab_loss_pair_tcgen05<MODE>;
   static PerDeviceOnce once;
   cudaError_t err = per_device_once(once, [&](int) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
@@ -1358,7 +1489,7 @@ cudaError_t launch_pairs(const VocabLossParams& p, int tiles, int sm_count, cuda
   if (err != cudaSuccess) return err;
   const int most = sm_count / 2 > 0 ? sm_count / 2 : 1;
   const int workers = tiles < most ? (tiles > 0 ? tiles : 1) : most;
-  return launch_kernel(kernel, dim3(2 * workers), dim3(threads(GRAD)), kSmemBytes, stream, p, 2u);
+  return launch_kernel(kernel, dim3(2 * workers), dim3(threads(MODE)), kSmemBytes, stream, p, 2u);
 }
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
@@ -1393,14 +1524,14 @@ ForwardPlan forward_plan(int rows, int vocab, int hidden, int sm_count) {
     if (best < 0 || cost < best) { best = cost; f.block_n = bn; }
   }
   f.tiles_n = ceil_div(vocab, f.block_n);
-  f.part_pitch = groups(false) * f.tiles_n;
+  f.part_pitch = groups(kForward) * f.tiles_n;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += whole_lines(bytes); return here; };
   f.count = take(256);
   f.row_of = take(f.row_pitch * 4);
   f.row_label = take(f.row_pitch * 4);
   f.label_logit = take(f.row_pitch * 4);
-  const size_t parts_of_row = rows <= kFewRows ? kFewPartCtas : static_cast<size_t>(ceil_div(vocab, kHalf)) * groups(false);   // (for the narrowest tiles)
+  const size_t parts_of_row = rows <= kFewRows ? kFewPartCtas : static_cast<size_t>(ceil_div(vocab, kHalf)) * groups(kForward);   // (for the narrowest tiles)
   f.parts = take(static_cast<size_t>(f.row_pitch) * parts_of_row * sizeof(float2));
   f.gathered = take(f.gather ? static_cast<size_t>(f.row_pitch) * hidden * 2 : 0);
   f.bytes = at;
@@ -1482,7 +1613,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
   if (c.rows <= kFewRows) {
     VocabFewParams w;
     memset(&w, 0, sizeof(w));
-    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.cut_off = kCutOff * c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
+    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
     w.label_logit = at<float>(ws, f.label_logit); w.parts = at<float2>(ws, f.parts);
     if ((e = few_maps(c, &w)) != cudaSuccess) return e;
     VocabJoinParams j;
@@ -1504,7 +1635,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
   }
   VocabLossParams p;
   memset(&p, 0, sizeof(p));
-  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.cut_off = kCutOff * c.hidden; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = f.block_n; p.block_h = kTile; p.bias = c.bias;
   p.labels = f.gather ? at<int32_t>(ws, f.row_label) : c.labels;
   p.count = f.gather ? at<int32_t>(ws, f.count) : nullptr;
   p.n_tiles = f.tiles_n;
@@ -1515,7 +1646,7 @@ cudaError_t launch_vocab_loss(const VocabLossCall& c, int sm_count, cudaStream_t
       (e = encode_matrix_map(&p.x_k[1], at<bf16>(ws, f.gathered), f.row_pitch, c.hidden, static_cast<int64_t>(c.hidden) * 2, kHalf, 64, false)) != cudaSuccess)
     return e;
   if ((e = encode_matrix_map(&p.w_k, c.w, c.vocab, c.hidden, c.w_stride * 2, f.block_n / 2, 64, false)) != cudaSuccess) return e;
-  if ((e = launch_pairs<false>(p, static_cast<int>(f.row_pitch / kTile) * f.tiles_n, sm_count, stream)) != cudaSuccess) return e;
+  if ((e = launch_pairs<kForward>(p, static_cast<int>(f.row_pitch / kTile) * f.tiles_n, sm_count, stream)) != cudaSuccess) return e;
   VocabJoinParams j;
   memset(&j, 0, sizeof(j));
   j.labels = p.labels; j.count = p.count; j.row_of = f.gather ? at<int32_t>(ws, f.row_of) : nullptr; j.parts = p.parts;
@@ -1547,7 +1678,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   const bool products = c.dx != nullptr || c.dw != nullptr;
   VocabLossParams p;
   memset(&p, 0, sizeof(p));
-  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.cut_off = kCutOff * c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias; p.status = c.status;
+  p.rows = c.rows; p.vocab = c.vocab; p.hidden = c.hidden; p.block_n = kTile; p.block_h = f.block_h; p.bias = c.bias; p.status = c.status;
   p.dx_sums = at<float>(ws, f.dx);
   p.want_x = c.dx != nullptr ? 1 : 0; p.want_w = c.dw != nullptr ? 1 : 0; p.accumulate = c.accumulate; p.n_tiles = ceil_div(c.hidden, f.block_h);
   p.dw = c.dw; p.dw_stride = c.dw_stride;
@@ -1556,7 +1687,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   if (f.few) {
     VocabFewParams w;
     memset(&w, 0, sizeof(w));
-    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.cut_off = kCutOff * c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
+    w.rows = c.rows; w.vocab = c.vocab; w.hidden = c.hidden; w.bias = c.bias; w.labels = c.labels; w.status = c.status;
     w.lse = c.lse; w.grad_loss = c.grad_loss; w.x = c.x; w.x_stride = c.x_stride; w.x_clean = c.dw != nullptr ? gathered : nullptr;
     w.g = g; w.g_pitch = f.g_pitch; w.db = c.db; w.accumulate = c.accumulate; w.row_residual = at<float>(ws, f.row_residual);
     w.counter = at<uint32_t>(ws, f.counters); w.two_terms = at<int32_t>(ws, f.two_terms);
@@ -1571,10 +1702,10 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
       return e;
     p.x_mn[1] = p.x_mn[0];
     p.x_k[0] = p.w_k = p.w_mn;      // (of kind 0, which has no tiles here)
-    p.by_words = 1; p.two_terms = w.two_terms; p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.counter = w.counter;
+    p.two_terms = w.two_terms; p.row_pitch = static_cast<int>(f.row_pitch); p.ranges = f.ranges; p.counter = w.counter;
     p.range_blocks = ceil_div(ceil_div(c.vocab, 64), f.ranges);
     const int tiles = p.n_tiles * (f.ranges + ceil_div(c.vocab, kTile));
-    if ((e = launch_pairs<true>(p, tiles, sm_count, stream)) != cudaSuccess || c.dx == nullptr) return e;
+    if ((e = launch_pairs<kProducts>(p, tiles, sm_count, stream)) != cudaSuccess || c.dx == nullptr) return e;
     return launch_kernel(vocab_finish_kernel, dim3(dx_ctas), dim3(kJoinThreads), 0, stream, d);
   }
 
@@ -1610,7 +1741,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   for (int j = 0; j <= f.pieces && (j < f.pieces || products); ++j) {
     p.work = r.work + j;
     p.counter = r.counters + j;
-    if ((e = launch_pairs<true>(p, sm_count, sm_count, stream)) != cudaSuccess) return e;
+    if ((e = launch_pairs<kGradient>(p, sm_count, sm_count, stream)) != cudaSuccess) return e;
   }
   if (c.dx == nullptr && c.db == nullptr) return cudaSuccess;
   d.row_of = r.row_of; d.labels = r.row_label; d.work = r.work; d.bias_parts = p.bias_parts; d.db_ctas = c.db != nullptr ? ceil_div(c.vocab, 32) : 0;
