@@ -173,8 +173,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) token_sort_kernel(const __gri
       for (int64_t i = static_cast<int64_t>(fill) * kSortThreads + tid; i < n; i += static_cast<int64_t>(n_fill) * kSortThreads)
         flat[i] = make_uint4(0, 0, 0, 0);
     } else {
-      for (int v = fill * kSortWarps + warp; v < p.vocab; v += n_fill * kSortWarps)
-        for (int c = lane; c < p.hidden; c += 32) table[static_cast<int64_t>(v) * p.table_stride + c] = O(0.f);
+      // (in 64 bits: the last step of a table of nearly 2^31 rows goes beyond them)
+      for (int64_t v = fill * kSortWarps + warp; v < p.vocab; v += n_fill * kSortWarps)
+        for (int c = lane; c < p.hidden; c += 32) table[v * p.table_stride + c] = O(0.f);
     }
     return;
   }

@@ -197,3 +197,18 @@ def test_binding_refusals():
     for args in [(ids, out, table, ws[:-256]), (ids, out[:, :8], table, ws), (ids, out, table, ws[1:]), (ids.cpu(), out, table, ws)]:
         with pytest.raises(mt.MTError):
             mt.mt_kernel_embedding_grad(*args)
+
+
+def test_zeros_of_a_table_of_nearly_as_many_rows_as_there_are_ids():
+    """Rows counted beyond 32 bits: the step behind the last row of a table of 2^31 - 1 must not come back in front of it."""
+    vocab, guard = 2 ** 31 - 1, 1 << 20
+    memory = torch.ones(guard + vocab, dtype=torch.bfloat16, device="cuda")
+    table = memory[guard:].view(vocab, 1)
+    ids = torch.arange(0, 1500, dtype=torch.int64) * 1_400_000
+    ids[-3:] = torch.tensor([vocab - 1, vocab - 2, vocab - 4673])
+    dy = (1.0 + torch.arange(1500) % 7).bfloat16().cuda()
+    ws = torch.empty(mt.mt_kernel_embedding_grad_workspace(1500, vocab, 1), dtype=torch.uint8, device="cuda")
+    mt.mt_kernel_embedding_grad(ids.int().cuda(), dy.view(1500, 1), table, ws)
+    torch.cuda.synchronize()
+    assert bool((memory[:guard] == 1.0).all())
+    assert torch.equal(table[ids.cuda(), 0], dy) and int(torch.count_nonzero(table)) == 1500
