@@ -262,6 +262,7 @@ class _Torch:
 
 
 _torch: Optional[_Torch] = None
+_MOST = 2 ** 31 - 1          # what a size of the library holds: ctypes would keep the low 32 bits of more without a word
 
 
 def _begin(where: str, stream):
@@ -287,6 +288,8 @@ def _matrix(where: str, device: int, t, rows: int, cols: int):
         raise _elsewhere(where, t, device)
     if t.shape != (rows, cols):
         raise MTError(-2, where, f"expected a {rows} x {cols} tensor, got {tuple(t.shape)}")
+    if rows > _MOST or cols > _MOST:
+        raise MTError(-2, where, f"{rows} x {cols}: sizes are below 2^31")
     dtype = _torch.dtypes.get(t.dtype)
     if dtype is None:
         raise MTError(-7, where, f"dtype {t.dtype}")
@@ -310,6 +313,8 @@ def _vector(where: str, device: int, t, n: int, dtype) -> int:
         return 0
     if t.get_device() != device:
         raise _elsewhere(where, t, device)
+    if n > _MOST:
+        raise MTError(-2, where, f"{n} elements: sizes are below 2^31")
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise MTError(-1, where, f"expected {n} contiguous elements of {dtype}, got {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
@@ -334,6 +339,10 @@ def _status_word(where: str, device: int, t) -> int:
     return t.data_ptr()
 
 
+def _sizes_fit(*sizes: int) -> bool:
+    return all(-_MOST <= n <= _MOST for n in sizes)
+
+
 def mt_kernel_embedding_lookup(ids, table, out, scale: float = 1.0, status=None, stream=None) -> None:
     """out[t] = scale * table[ids[t]] (ids int32 of any shape, out [ids.numel(), hidden]); zeros for ids < 0."""
     where = "mt_kernel_embedding_lookup"
@@ -348,7 +357,7 @@ def mt_kernel_embedding_lookup(ids, table, out, scale: float = 1.0, status=None,
 
 
 def mt_kernel_embedding_grad_workspace(tokens: int, vocab: int, hidden: int) -> int:
-    return lib().mt_kernel_embedding_grad_workspace(tokens, vocab, hidden)
+    return lib().mt_kernel_embedding_grad_workspace(tokens, vocab, hidden) if _sizes_fit(tokens, vocab, hidden) else 0
 
 
 def mt_kernel_embedding_grad(ids, grad_out, grad_table, workspace, scale: float = 1.0, padding_id: int = -1,
@@ -356,6 +365,8 @@ def mt_kernel_embedding_grad(ids, grad_out, grad_table, workspace, scale: float 
     """grad_table[v] = scale * sum of grad_out[t] over ids[t] == v, zeros where there is none; or added to grad_table."""
     where = "mt_kernel_embedding_grad"
     torch, device, stream = _begin(where, stream)
+    if not _sizes_fit(padding_id):
+        raise MTError(-1, where, f"padding_id {padding_id} is no id")
     tokens, (vocab, hidden) = ids.numel(), grad_table.shape
     grad_ptr, grad_dtype, grad_stride = _matrix(where, device, grad_out, tokens, hidden)
     table_ptr, table_dtype, table_stride = _matrix(where, device, grad_table, vocab, hidden)
@@ -391,7 +402,7 @@ def mt_kernel_dropout(x, y, p: float, seed: int, counter: int = 0, residual=None
 
 
 def mt_kernel_vocab_loss_workspace(rows: int, vocab: int, hidden: int) -> int:
-    return lib().mt_kernel_vocab_loss_workspace(rows, vocab, hidden)
+    return lib().mt_kernel_vocab_loss_workspace(rows, vocab, hidden) if _sizes_fit(rows, vocab, hidden) else 0
 
 
 def mt_kernel_vocab_loss(x, w, bias, labels, loss, lse, workspace, status=None, stream=None) -> None:
@@ -410,7 +421,7 @@ def mt_kernel_vocab_loss(x, w, bias, labels, loss, lse, workspace, status=None, 
 
 
 def mt_kernel_vocab_loss_grad_workspace(rows: int, vocab: int, hidden: int) -> int:
-    return lib().mt_kernel_vocab_loss_grad_workspace(rows, vocab, hidden)
+    return lib().mt_kernel_vocab_loss_grad_workspace(rows, vocab, hidden) if _sizes_fit(rows, vocab, hidden) else 0
 
 
 def mt_kernel_vocab_loss_grad(x, w, bias, labels, lse, grad_loss, grad_x, grad_w, grad_bias, workspace, accumulate: bool = False, status=None,
