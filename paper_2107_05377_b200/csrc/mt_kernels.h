@@ -499,7 +499,7 @@ struct VocabLossParams {
   const int32_t* labels;       // of the rows in use
   const int32_t* count;        // forward: rows in use (or null: rows)
   const VocabWork* work;       // backward, of this launch (null: few rows, all of it as given below)
-  const float4* row_shift;     // backward, of every row: its lse, its weight's logarithm and its weight
+  const float2* row_shift;     // backward, of every row: its lse and its weight
   float* row_residual;         // backward: what rounding takes from the label's entry of g
   float* label_logit;          // forward: of every row; and (largest logit, sum) of every half tile [row][part_pitch]
   float2* parts;
@@ -553,7 +553,7 @@ struct VocabRowsParams {
   uint32_t* counters;          // set to zero
   int32_t* row_of;             // caller's row of a row in use
   int32_t* row_label;
-  float4* row_shift;           // backward: see VocabLossParams
+  float2* row_shift;           // backward: see VocabLossParams
   bf16* gathered;
   bf16* dx;                    // backward: zeros for rows without a label; or null
   int64_t dx_stride;

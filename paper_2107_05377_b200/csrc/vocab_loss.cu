@@ -292,6 +292,11 @@ __device__ __forceinline__ float column_sums(float (&c)[32], int lane) {
   return c[0];
 }
 
+// exp(z - lse).  (z - lse first: what is rounded is the size of the exponent and not of its terms, in an error of its own for every entry; and
+// both may be at the lowest number.)  The row's weight is a factor: its logarithm within the exponent would be rounded at a size of its own,
+// 1e-6 of the weight at a weight of 1e-12.
+__device__ __forceinline__ float probability(float z, float lse) { return ex2_approx((z - lse) * kLog2e); }
+
 template <Mode MODE>
 __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
   constexpr bool GRAD = MODE != kForward;
@@ -637,7 +642,7 @@ __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(cons
         const bool row_counts = row < rows;
         if (MODE != kProducts && t.kind == 0) {
           const int label = row_counts ? p.labels[row] : -1;
-          const float4 shift = row_counts ? p.row_shift[row] : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float2 shift = row_counts ? p.row_shift[row] : make_float2(0.f, 0.f);   // lse, weight
           // The logits of this warp's rows and columns, in registers: the last of their accumulators is free before anything is done with them.
           const int n0 = t.n * p.block_n;                 // in the piece
           // (what anything below looks at: in whole k-blocks of the products that sum over columns and over rows)
@@ -662,19 +667,14 @@ __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(cons
             const int col = work.col0 + local;
             float (&g)[32] = z[i];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) g[j] = ex2_approx(fmaf(g[j] - shift.x, kLog2e, shift.y));
-            if (__any_sync(0xffffffffu, shift.z < 0.f)) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) g[j] = shift.z < 0.f ? -g[j] : g[j];
-            }
+            for (int j = 0; j < 32; ++j) g[j] = shift.y * probability(g[j], shift.x);
             const int at = label - col;
-            const bool hit = __any_sync(0xffffffffu, at >= 0 && at < 32);
-            if (hit) {
+            if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
               float mine = 0.f;
 #pragma unroll
               for (int j = 0; j < 32; ++j) {
                 if (j == at) {
-                  g[j] -= shift.z;
+                  g[j] -= shift.y;
                   mine = g[j];
                 }
               }
@@ -806,11 +806,6 @@ __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(cons
   }
 }
 
-// What a row's entries of g need: |weight| exp(z - lse) = 2^((z - lse) log2 e + log2 |weight|), and the weight, whose sign is put in
-// afterwards.  (z - lse first: what is rounded is the size of the exponent and not of its terms, in an error of its own for every entry; and
-// both may be at the lowest number.)
-__device__ __forceinline__ float4 weighted_shift(float lse, float weight) { return make_float4(lse, log2f(fabsf(weight)), weight, 0.f); }
-
 // ---- few rows ------------------------------------------------------------------------------------
 
 // Up to 128 rows the products are taken turned: 128 words are the rows (lanes) of an accumulator and the rows of x, rounded up to sixteen,
@@ -870,10 +865,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(book + 8 * (2 * kFewMaxStages + 6 * kFewAccs));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_label = reinterpret_cast<int*>(book + 512);                    // of every row; -1 where it takes no part
-  float4* s_row = reinterpret_cast<float4*>(book + 512 + 512);          // (backward) weighted_shift
-  float2* s_part = reinterpret_cast<float2*>(book + 512 + 512 + 2048);  // (forward) [quarter][row]
+  float2* s_row = reinterpret_cast<float2*>(book + 512 + 512);          // (backward) lse, weight
+  float2* s_part = reinterpret_cast<float2*>(book + 512 + 512 + 1024);  // (forward) [quarter][row]
   float* s_db = reinterpret_cast<float*>(s_part);                       // (backward) [accumulator][quarter][word]
-  static_assert(8 * (2 * kFewMaxStages + 6 * kFewAccs) + 8 <= 512 && 512 + 512 + 2048 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
+  static_assert(8 * (2 * kFewMaxStages + 6 * kFewAccs) + 8 <= 512 && 512 + 512 + 1024 + 4 * kFewRows * 8 <= kFewBook, "bookkeeping");
   static_assert(kFewAccs * 4 * 32 * 4 <= 4 * kFewRows * 8, "sums of db");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -984,7 +979,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
       if (label >= p.vocab) label = -1;
       s_label[first] = label;
       if (GRAD)
-        s_row[first] = label >= 0 ? weighted_shift(p.lse[first], p.grad_loss != nullptr ? p.grad_loss[first] : 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
+        s_row[first] = label >= 0 ? make_float2(p.lse[first], p.grad_loss != nullptr ? p.grad_loss[first] : 1.f) : make_float2(0.f, 0.f);
     }
     // (the epilogue warps; nothing that can give up comes before it)
     asm volatile("bar.sync 1, %0;" ::"n"(32 * kFewWarps) : "memory");
@@ -1081,19 +1076,14 @@ __global__ void __launch_bounds__(kFewThreads, 1) vocab_few_tcgen05(const __grid
           const uint32_t counts = __ballot_sync(0xffffffffu, my_label >= 0);
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
-            const float2 shift = *reinterpret_cast<const float2*>(&s_row[i * 32 + j]);
-            z[j] = ex2_approx(fmaf(z[j] - shift.x, kLog2e, shift.y));
-          }
-          const uint32_t negative = __ballot_sync(0xffffffffu, s_row[i * 32 + lane].z < 0.f);
-          if (negative != 0) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) z[j] = ((negative >> j) & 1u) ? -z[j] : z[j];
+            const float2 shift = s_row[i * 32 + j];
+            z[j] = shift.y * probability(z[j], shift.x);
           }
           if (hits != 0) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
               if (((hits >> j) & 1u) && s_label[i * 32 + j] == word) {
-                z[j] -= s_row[i * 32 + j].z;
+                z[j] -= s_row[i * 32 + j].y;
                 p.row_residual[i * 32 + j] = z[j] - __bfloat162float(__float2bfloat16_rn(z[j]));   // what rounding takes from the label's entry
               }
             }
@@ -1261,7 +1251,7 @@ __global__ void __launch_bounds__(kRowsThreads) vocab_rows_kernel(const __grid_c
       if (has) {
         p.row_of[place] = r;
         p.row_label[place] = p.labels[r];
-        if (p.row_shift != nullptr) p.row_shift[place] = weighted_shift(p.lse[r], p.grad_loss != nullptr ? p.grad_loss[r] : 1.f);
+        if (p.row_shift != nullptr) p.row_shift[place] = make_float2(p.lse[r], p.grad_loss != nullptr ? p.grad_loss[r] : 1.f);
       } else if (p.loss_out != nullptr) {
         p.loss_out[r] = 0.f;
         p.lse_out[r] = 0.f;
@@ -1570,7 +1560,7 @@ GradPlan grad_plan(int rows, int vocab, int hidden) {
   f.counters = take((static_cast<size_t>(f.pieces) + 1) * 4);
   f.row_of = take(f.row_pitch * 4);
   f.row_label = take(f.row_pitch * 4);
-  f.row_shift = take(f.row_pitch * 16);
+  f.row_shift = take(f.row_pitch * 8);
   f.row_residual = take(f.row_pitch * 4);
   f.gathered = take(static_cast<size_t>(f.row_pitch) * hidden * 2);
   f.g = take(static_cast<size_t>(f.buffers) * (f.few ? 2 * f.g_pitch : f.row_pitch) * f.piece * 2);
@@ -1713,7 +1703,7 @@ cudaError_t launch_vocab_loss_grad(const VocabLossCall& c, int sm_count, cudaStr
   memset(&r, 0, sizeof(r));
   r.labels = c.labels; r.x = c.x; r.x_stride = c.x_stride; r.rows = c.rows; r.vocab = c.vocab; r.hidden = c.hidden;
   r.count = at<int32_t>(ws, f.count); r.row_of = at<int32_t>(ws, f.row_of); r.row_label = at<int32_t>(ws, f.row_label);
-  r.row_shift = at<float4>(ws, f.row_shift); r.dx = c.dx; r.dx_stride = c.dx_stride;
+  r.row_shift = at<float2>(ws, f.row_shift); r.dx = c.dx; r.dx_stride = c.dx_stride;
   r.lse = c.lse; r.grad_loss = c.grad_loss; r.gathered = at<bf16>(ws, f.gathered);
   r.counters = at<uint32_t>(ws, f.counters); r.n_counters = f.pieces + 1; r.status = c.status;
   r.work = at<VocabWork>(ws, f.work); r.piece = f.piece; r.max_shift = f.max_shift; r.buffers = f.buffers; r.buffer_rows = static_cast<int>(f.row_pitch);

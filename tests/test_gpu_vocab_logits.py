@@ -90,3 +90,21 @@ def test_gradients_are_not_off_on_average(rows, hidden):
     db = backward(x, w, torch.from_numpy(z).float().cuda(), torch.full((rows,), 1.0 / rows, device="cuda"))[2]
     # (0.27 of half a step per 16 of 384 terms, and a tenth more; the lse is rounded, the exponential off by 2^-22)
     assert abs(float(db)) <= 0.3 * F32 * 24 * z.mean() + F32 * np.abs(z).max() + 2.0 ** -21
+
+
+@pytest.mark.parametrize("rows", [100, 300])
+@pytest.mark.parametrize("weight", [0.7 * 2.0 ** -12, -0.7 * 2.0 ** -12, 3e-12, 7e-25, -7e-25, 7e19])
+def test_a_weight_scales_the_gradient_whatever_its_size(rows, weight):
+    """Rows sure of their label: weight * (p - 1) with p near 1.  p is off by the exponential's 2^-22 and the product by half a step, so that the
+    gradient is off by as much of the weight, however far the weight is from one."""
+    x, w = torch.zeros(rows, 8, dtype=torch.bfloat16, device="cuda"), torch.randn(2, 8, device="cuda").bfloat16()
+    bias = torch.tensor([0.0, -10.0], device="cuda").bfloat16()
+    lse = np.float32(np.log1p(np.exp(-10.0)))
+    weight = np.float32(weight)
+    db = f64(backward(x, w, torch.full((rows,), float(lse), device="cuda"), torch.full((rows,), float(weight), device="cuda"), bias)[2])
+    want = rows * float(weight) * np.array([np.expm1(-float(lse)), np.exp(-10.0 - float(lse))])
+    bound = rows * abs(float(weight)) * (2.0 ** -22 + 2.0 ** -23) * np.array([1.0, np.exp(-10.0) * 8]) + (rows + 2) * F32 * np.abs(want)
+    assert (np.abs(db - want) <= bound).all()
+    # and none at all where the label has all of the probability
+    grads = backward(x, w[:1], torch.zeros(rows, device="cuda"), torch.full((rows,), float(weight), device="cuda"), bias[:1])
+    assert not any(g.any() for g in grads)
