@@ -2457,7 +2457,7 @@ int mt_kernel_embedding_lookup(const int32_t* d_ids, const void* d_table, void* 
     return MT_ERR_SHAPE;
   if (tokens == 0) return MT_OK;
   if (d_ids == nullptr || d_table == nullptr || d_out == nullptr || reinterpret_cast<uintptr_t>(d_ids) % 4 != 0 ||
-      misaligned(d_table, table_dtype) || misaligned(d_out, out_dtype))
+      misaligned(d_table, table_dtype) || misaligned(d_out, out_dtype) || misaligned(d_status, MT_DTYPE_F32))
     return MT_ERR_INVALID_ARG;
   LookupParams p;
   p.ids = d_ids; p.table = d_table; p.out = d_out; p.table_stride = table_stride; p.out_stride = out_stride;
@@ -2486,7 +2486,7 @@ int mt_kernel_embedding_grad(const int32_t* d_ids, const void* d_grad_out, void*
   if (tokens < 0 || tokens > kMaxTokens || vocab < 1 || hidden < 1 || hidden > kMaxColumns || grad_out_stride < hidden ||
       grad_table_stride < hidden)
     return MT_ERR_SHAPE;
-  if (d_grad_table == nullptr || misaligned(d_grad_table, grad_table_dtype)) return MT_ERR_INVALID_ARG;
+  if (d_grad_table == nullptr || misaligned(d_grad_table, grad_table_dtype) || misaligned(d_status, MT_DTYPE_F32)) return MT_ERR_INVALID_ARG;
   if (tokens > 0 && (d_ids == nullptr || d_grad_out == nullptr || reinterpret_cast<uintptr_t>(d_ids) % 4 != 0 ||
                      misaligned(d_grad_out, grad_out_dtype) || d_workspace == nullptr || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
                      workspace_bytes < mt_kernel_embedding_grad_workspace(tokens, vocab, hidden)))
@@ -2543,7 +2543,7 @@ int mt_kernel_vocab_loss(const void* d_x, const void* d_w, const void* d_bias, c
   if (rows == 0) return MT_OK;
   if (d_x == nullptr || d_w == nullptr || d_labels == nullptr || d_loss == nullptr || d_lse == nullptr || d_workspace == nullptr ||
       misaligned16({d_x, d_w, d_bias}) || misaligned(d_labels, MT_DTYPE_F32) || misaligned(d_loss, MT_DTYPE_F32) ||
-      misaligned(d_lse, MT_DTYPE_F32) || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
+      misaligned(d_lse, MT_DTYPE_F32) || misaligned(d_status, MT_DTYPE_F32) || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
       workspace_bytes < mt_kernel_vocab_loss_workspace(rows, vocab, hidden))
     return MT_ERR_INVALID_ARG;
   int sms = 0;
@@ -2576,7 +2576,7 @@ int mt_kernel_vocab_loss_grad(const void* d_x, const void* d_w, const void* d_bi
   }
   if (d_x == nullptr || d_w == nullptr || d_labels == nullptr || d_lse == nullptr || d_workspace == nullptr ||
       misaligned16({d_x, d_w, d_bias}) || misaligned(d_labels, MT_DTYPE_F32) || misaligned(d_lse, MT_DTYPE_F32) ||
-      misaligned(d_grad_loss, MT_DTYPE_F32) || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
+      misaligned(d_grad_loss, MT_DTYPE_F32) || misaligned(d_status, MT_DTYPE_F32) || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0 ||
       workspace_bytes < mt_kernel_vocab_loss_grad_workspace(rows, vocab, hidden))
     return MT_ERR_INVALID_ARG;
   int sms = 0;

@@ -90,3 +90,10 @@ def test_loss_workspaces(lib):
         assert 0 < size(1, 1, 8) <= size(1, 30522, 768) <= size(256, 30522, 768)
     # the logits are not kept: a fraction of their fp32 size, in bf16 pieces
     assert lib.mt_kernel_vocab_loss_grad_workspace(8192, 131072, 1024) < 8192 * 131072 * 4 / 8
+
+
+@pytest.mark.parametrize("name,base", [("mt_kernel_embedding_lookup", LOOKUP), ("mt_kernel_embedding_grad", GRAD), ("mt_kernel_vocab_loss", LOSS),
+                                       ("mt_kernel_vocab_loss_grad", LOSS_GRAD)])
+def test_status_words_that_are_not_aligned(lib, name, base):
+    for off in (1, 2, 3):
+        assert call(lib, name, base, status=A + off) == INVALID
