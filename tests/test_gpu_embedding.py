@@ -212,3 +212,30 @@ def test_zeros_of_a_table_of_nearly_as_many_rows_as_there_are_ids():
     torch.cuda.synchronize()
     assert bool((memory[:guard] == 1.0).all())
     assert torch.equal(table[ids.cuda(), 0], dy) and int(torch.count_nonzero(table)) == 1500
+
+
+@pytest.mark.parametrize("tokens,vocab", [(140001, 70000), (300000, 513)])
+def test_gradient_of_lists_that_no_warp_holds(tokens, vocab):
+    """More than 131072 tokens: a warp of the sort has more of them than its registers hold from the count to their places."""
+    grad_case(skewed(tokens, vocab, tokens), vocab, 8, torch.float32, torch.float32)
+    grad_case(np.full(tokens, 4), 6, 8, torch.bfloat16, torch.float32)
+
+
+@pytest.mark.parametrize("tokens", [1025, 1500, 2048, 2049, 30000])
+@pytest.mark.parametrize("vocab", [300_000, 2 ** 27 + 5])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_sort_in_three_and_four_passes(tokens, vocab, accumulate):
+    """Up to 2048 tokens one CTA sorts in place, in shared memory; beyond, a cluster from one list to the other."""
+    rng = np.random.default_rng(tokens)
+    named = rng.integers(0, vocab, 200)
+    ids = np.where(rng.uniform(size=tokens) < 0.5, rng.integers(0, vocab, tokens), named[rng.integers(0, 200, tokens)])
+    ids[::50], ids[1::50] = -1, vocab - 1
+    dy = torch.from_numpy(rng.integers(-8, 9, tokens)).float().cuda()            # (sums of small integers: exact in any order)
+    table = torch.full((vocab, 1), 0.5, device="cuda")
+    ws = torch.full((mt.mt_kernel_embedding_grad_workspace(tokens, vocab, 1),), 0xFF, dtype=torch.uint8, device="cuda")
+    mt.mt_kernel_embedding_grad(torch.from_numpy(ids.astype(np.int32)).cuda(), dy.view(-1, 1), table, ws, accumulate=accumulate)
+    torch.cuda.synchronize()
+    there = torch.from_numpy(ids >= 0).cuda()
+    want = torch.full((vocab,), 0.5 if accumulate else 0.0, dtype=torch.float64, device="cuda")
+    want.index_add_(0, torch.from_numpy(ids).cuda()[there], dy.double()[there])
+    assert torch.equal(table[:, 0].double(), want)

@@ -147,3 +147,25 @@ def test_equal_bits_on_two_streams_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         c.check(out)
+
+
+@pytest.mark.parametrize("rows", [0, 5, 300])
+def test_rows_of_the_table_gigabytes_apart(rows):
+    """A stride of more than 2^31 bytes, of the table and of its gradient, with and without rows."""
+    vocab, hidden, stride = 2, 24, 2 ** 30 + 8
+    w_memory, dw_memory = (torch.zeros(stride + hidden, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = Case(rows, vocab, hidden, rows)
+    w = torch.as_strided(w_memory, (vocab, hidden), (stride, 1))
+    w.copy_(c.w)
+    c.w = w
+    out = c.outputs()
+    out[1] = torch.as_strided(dw_memory, (vocab, hidden), (stride, 1))
+    out[1].fill_(1.0)
+    dw_memory[hidden] = 3.0
+    c.run(out, c.workspace())
+    torch.cuda.synchronize()
+    if rows:
+        c.check(out)
+    else:
+        assert not out[1].any() and not out[2].any()
+    assert float(dw_memory[hidden]) == 3.0 and float(dw_memory[hidden + 1:stride].abs().max()) == 0.0

@@ -148,3 +148,13 @@ def test_first_calls_of_a_process_may_be_captured():
             "g.replay(); torch.cuda.synchronize(); s.check(0); t.check(0); print('captured')" % (ROOT, os.path.join(ROOT, "tests")))
     out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=300)
     assert out.returncode == 0 and "captured" in out.stdout, out.stderr[-2000:]
+
+
+def test_first_calls_of_a_process_with_a_sort_may_be_captured():
+    """Token lists that one CTA and that a cluster of sixteen sorts, whose launch asks the device what fits."""
+    code = ("import torch, sys; sys.path[:0] = [%r, %r]; from test_gpu_vocab_step import Step; s = Step(1500, 900, 72, 0.5); t = Step(6000, 900, 72, 0.3)\n"
+            "torch.cuda.synchronize(); g = torch.cuda.CUDAGraph()\n"
+            "with torch.cuda.graph(g):\n    t.run(); s.run()\n"
+            "g.replay(); torch.cuda.synchronize(); s.check(0); t.check(0); print('captured')" % (ROOT, os.path.join(ROOT, "tests")))
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=300)
+    assert out.returncode == 0 and "captured" in out.stdout, out.stderr[-2000:]
