@@ -39,13 +39,19 @@ constexpr int kStageB = kHalf * 128;
 // there.  The first two have eight epilogue warps, which keep the 128 logits that each thread has of a tile in registers; the tiles of
 // the third are so short (two k-blocks) that their epilogue is what they take, and sixteen warps share it.
 enum Mode { kForward, kGradient, kProducts };
-__host__ __device__ constexpr int epilogue_warps(Mode mode) { return mode == kProducts ? 16 : 8; }
+__host__ __device__ constexpr int epilogue_warps(Mode mode) { return mode == kProducts ? 16 : 12; }
 __host__ __device__ constexpr int first_epilogue_warp(Mode mode) { return mode == kProducts ? 2 : 4; }
 __host__ __device__ constexpr int threads(Mode mode) { return 32 * (first_epilogue_warp(mode) + epilogue_warps(mode)); }
 __host__ __device__ constexpr int groups(Mode mode) { return epilogue_warps(mode) / 4; }   // of the same rows: they share the columns
-// Registers of a thread, by warpgroup: the producer's, the MMA issuer's and the epilogue's, of the 168 that each of 384 threads starts with.
-constexpr int kIssueRegs = 56, kEpilogueRegs = 224;
-static_assert(128 * kIssueRegs + 256 * kEpilogueRegs <= 384 * 168, "within what the CTA was launched with");
+__host__ __device__ constexpr int blocks(Mode mode) { return (8 + groups(mode) - 1) / groups(mode); }   // of 32 columns of a tile, for a thread
+// Registers of a thread: of the 120 that each of 512 threads of the first two starts with, the warpgroup of the producer and the MMA issuer
+// gives up, and the epilogue's take (a share that is not there would be waited for without end: launch_pairs looks at what the kernel has).  The rest
+// of the SM's are room for a CTA of the small kernel behind this one, which then starts while this one ends.
+constexpr int kPairRegs = 128, kIssueRegs = 56, kEpilogueRegs = 152;
+__host__ __device__ constexpr int registers_needed(Mode mode) {
+  return mode == kProducts ? 0 : 32 * (first_epilogue_warp(mode) * kIssueRegs + epilogue_warps(mode) * kEpilogueRegs);
+}
+static_assert(registers_needed(kForward) <= kPairRegs * threads(kForward) && registers_needed(kGradient) <= kPairRegs * threads(kGradient), "");
 constexpr int kBook = 1024;
 constexpr int kSlots = 4;                  // tiles announced ahead
 constexpr uint32_t kTmemCols = 512;
@@ -244,8 +250,12 @@ __device__ __forceinline__ void put_sums(const float (&sum)[BLOCKS][32], uint32_
   tmem_st_wait();
 }
 
-// The bias of a thread's words, blocks of 32 from `col` on, `step` apart: all asked for before the first is used (block by block it took 700
-// clocks a block), and added to their logits.  At the vocabulary's end a lane reads that of one word per block, -inf behind the last word.
+// Something read for nothing but to be in L1 (a prefetch leaves nothing there): a tile's bias, which its threads then take from there (from L2, block
+// by block, it took 700 clocks a block).
+__device__ __forceinline__ void touch(const bf16* p) { asm volatile("{\n\t.reg .b16 t;\n\tld.global.nc.b16 t, [%0];\n\t}" ::"l"(p)); }
+
+// The bias of a thread's words, blocks of 32 from `col` on, `step` apart, added to their logits.  At the vocabulary's end a lane reads that of
+// one word per block, -inf behind the last word.
 template <int BLOCKS>
 __device__ __forceinline__ void add_bias(const bf16* bias, int col, int step, int vocab, int lane, float (&z)[BLOCKS][32]) {
   if (col + (BLOCKS - 1) * step + 32 > vocab) {
@@ -257,22 +267,19 @@ __device__ __forceinline__ void add_bias(const bf16* bias, int col, int step, in
       for (int j = 0; j < 32; ++j) z[i][j] += __shfl_sync(0xffffffffu, b, j);
     }
   } else if (bias != nullptr) {
-    uint4 v[BLOCKS][4];
 #pragma unroll
-    for (int i = 0; i < BLOCKS; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[i][q] = __ldg(reinterpret_cast<const uint4*>(bias + col + i * step) + q);
-#pragma unroll
-    for (int i = 0; i < BLOCKS; ++i)
+    for (int i = 0; i < BLOCKS; ++i) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint32_t w[4] = {v[i][q].x, v[i][q].y, v[i][q].z, v[i][q].w};
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(bias + col + i * step) + q);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           z[i][q * 8 + 2 * j] += bf16_lo(w[j]);
           z[i][q * 8 + 2 * j + 1] += bf16_hi(w[j]);
         }
       }
+    }
   }
 }
 
@@ -298,7 +305,7 @@ __device__ __forceinline__ float column_sums(float (&c)[32], int lane) {
 __device__ __forceinline__ float probability(float z, float lse) { return ex2_approx((z - lse) * kLog2e); }
 
 template <Mode MODE>
-__global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
+__global__ void __maxnreg__(MODE == kProducts ? 96 : kPairRegs) vocab_loss_pair_tcgen05(const __grid_constant__ VocabLossParams p) {
   constexpr bool GRAD = MODE != kForward;
   constexpr int STAGES = kStages;
   constexpr int EPILOGUE_WARPS = epilogue_warps(MODE), GROUPS = groups(MODE);
@@ -552,7 +559,7 @@ __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(cons
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     };
     if constexpr (MODE == kForward) {
-      constexpr int BLOCKS = kTile / 32 / GROUPS;
+      constexpr int BLOCKS = blocks(MODE);
       float z[BLOCKS][32];
       bool taken = false;                               // the first sum of the tile's logits is there already
       auto take = [&](int i, int end) {
@@ -566,7 +573,7 @@ __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(cons
         const int row = t.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 + lane, col = t.n * p.block_n + lane * 16;
         next_label = row < rows ? p.labels[row] : -1;
         if (p.bias != nullptr && lane < 16 && col < p.vocab)
-          asm volatile("{\n\t.reg .b16 t;\n\tld.global.nc.b16 t, [%0];\n\t}" ::"l"(p.bias + col));
+          touch(p.bias + col);
         return true;
       };
       for (bool more = next_tile(true); more;) {
@@ -647,8 +654,8 @@ __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(cons
           const int n0 = t.n * p.block_n;                 // in the piece
           // (what anything below looks at: in whole k-blocks of the products that sum over columns and over rows)
           const int columns = m0 >= (rows + 63) / 64 * 64 ? 0 : min(p.block_n, (work.cols - n0 + 63) / 64 * 64);
-          float z[kTile / 32 / GROUPS][32] = {};
-          add_bias(p.bias, work.col0 + n0 + group * 32, 32 * GROUPS, p.vocab, lane, z);
+          float z[blocks(MODE)][32] = {};
+          if (p.bias != nullptr && lane < 16 && work.col0 + n0 + lane * 16 < p.vocab) touch(p.bias + work.col0 + n0 + lane * 16);
           bool ok = true;
           for (int i = 0; ok && i < sums; ++i) {
             if (!(ok = wait_sum())) break;
@@ -657,10 +664,11 @@ __global__ void __launch_bounds__(threads(MODE), 1) vocab_loss_pair_tcgen05(cons
             leave_sum();
           }
           if (!ok) break;
+          add_bias(p.bias, work.col0 + n0 + group * 32, 32 * GROUPS, p.vocab, lane, z);
           const bool whole = __all_sync(0xffffffffu, row_counts);
           bf16* g_out = p.g + static_cast<int64_t>(work.g_row0 + m0 + (lane & ~3)) * g_pitch + (lane & 3) * 8;
 #pragma unroll
-          for (int i = 0; i < kTile / 32 / GROUPS; ++i) {
+          for (int i = 0; i < blocks(MODE); ++i) {
             const int c = group * 32 + 32 * GROUPS * i;
             if (c >= columns) break;
             const int local = n0 + c;
@@ -1474,6 +1482,10 @@ cudaError_t launch_pairs(const VocabLossParams& p, int tiles, int sm_count, cuda
   auto kernel = vocab_loss_pair_tcgen05<MODE>;
   static PerDeviceOnce once;
   cudaError_t err = per_device_once(once, [&](int) {
+    cudaFuncAttributes has;
+    cudaError_t e = cudaFuncGetAttributes(&has, kernel);
+    if (e != cudaSuccess) return e;
+    if (has.numRegs * threads(MODE) < registers_needed(MODE)) return cudaErrorInvalidConfiguration;
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   });
   if (err != cudaSuccess) return err;
