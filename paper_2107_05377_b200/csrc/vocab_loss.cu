@@ -36,22 +36,22 @@ constexpr int kHalf = 128;                 // rows of a CTA
 constexpr int kStageA = kHalf * 128;       // bytes: 128 rows of 64 elements, or two boxes of 64 x 64
 constexpr int kStageB = kHalf * 128;
 // What a launch of the pair kernel is for: the forward pass, the gradient (all kinds of tiles), or the two products of few rows, whose g is
-// there.  The first two have eight epilogue warps, which keep the 128 logits that each thread has of a tile in registers; the tiles of
-// the third are so short (two k-blocks) that their epilogue is what they take, and sixteen warps share it.
+// there.  The first two have twelve epilogue warps, in three groups that share the columns, and keep the logits of a tile (up to 96 a thread) in
+// registers; the tiles of the third are so short (two k-blocks) that their epilogue is what they take, and sixteen warps share it.  (With eight
+// warps of 128 logits a thread: forward, 8192 rows x 30522 x 1024 385 us against 371, 4096 x 768 172 against 161; gradient 4096 x 768 588 against 575.)
 enum Mode { kForward, kGradient, kProducts };
 __host__ __device__ constexpr int epilogue_warps(Mode mode) { return mode == kProducts ? 16 : 12; }
 __host__ __device__ constexpr int first_epilogue_warp(Mode mode) { return mode == kProducts ? 2 : 4; }
 __host__ __device__ constexpr int threads(Mode mode) { return 32 * (first_epilogue_warp(mode) + epilogue_warps(mode)); }
 __host__ __device__ constexpr int groups(Mode mode) { return epilogue_warps(mode) / 4; }   // of the same rows: they share the columns
 __host__ __device__ constexpr int blocks(Mode mode) { return (8 + groups(mode) - 1) / groups(mode); }   // of 32 columns of a tile, for a thread
-// Registers of a thread: of the 120 that each of 512 threads of the first two starts with, the warpgroup of the producer and the MMA issuer
-// gives up, and the epilogue's take (a share that is not there would be waited for without end: launch_pairs looks at what the kernel has).  The rest
-// of the SM's are room for a CTA of the small kernel behind this one, which then starts while this one ends.
+// Registers of a thread: of the 128 that each of 512 threads of the first two starts with, the warpgroup of the producer and the MMA issuer
+// gives up, and the epilogue's take (a share that is not there would be waited for without end: launch_pairs looks at what the kernel has).
 constexpr int kPairRegs = 128, kIssueRegs = 56, kEpilogueRegs = 152;
 __host__ __device__ constexpr int registers_needed(Mode mode) {
   return mode == kProducts ? 0 : 32 * (first_epilogue_warp(mode) * kIssueRegs + epilogue_warps(mode) * kEpilogueRegs);
 }
-static_assert(registers_needed(kForward) <= kPairRegs * threads(kForward) && registers_needed(kGradient) <= kPairRegs * threads(kGradient), "");
+static_assert(registers_needed(kForward) <= kPairRegs * threads(kForward) && registers_needed(kGradient) <= kPairRegs * threads(kGradient), "shares");
 constexpr int kBook = 1024;
 constexpr int kSlots = 4;                  // tiles announced ahead
 constexpr uint32_t kTmemCols = 512;
@@ -207,8 +207,8 @@ __device__ __forceinline__ Tile find_tile(const VocabWork& w, int n_tiles, int k
 // at most this many k-blocks, each in an accumulator of its own, and joined in fp32, rounding to nearest, by the epilogue: what is cut off
 // is that of a logit of 256 (forward, up to 768 wide) or 384 terms whatever the width, and a sum that fp32 holds exactly comes out exactly.
 // Each further sum costs its tile a change of accumulators and a pass over one of them, some 1300 clocks, of which a wide tile hides most.
-// (Against one sum per tile: forward, 8192 rows x 30522 x 1024 in three sums 367 -> 385 us, 4096 x 768 in three 150 -> 173; gradient, 8192 x 1024 in
-// three 1340 -> 1372, 4096 x 768 in two 555 -> 588.  In sums of four k-blocks 1024 wide took 437 and 1417 us.)
+// (Against one sum per tile: forward, 8192 rows x 30522 x 1024 in three sums 363 -> 370 us, 4096 x 768 in three 150 -> 161; gradient, 8192 x 1024 in
+// three 1316 -> 1370, 4096 x 768 in two 560 -> 575.  Sums of four k-blocks at a width of 1024: forward 437, gradient 1417, both with eight warps.)
 __host__ __device__ constexpr int sum_blocks(bool grad, int k_blocks) { return !grad && k_blocks <= 12 ? 4 : 6; }
 
 // A sum of 32 columns from its accumulator, and one added to what is there.
