@@ -474,6 +474,9 @@ int mt_kernel_pooler_head_static(const void* d_hidden, const void* d_pool_w, con
  * length); rows themselves are contiguous.  A workspace is 256-byte aligned, of at least the size that its function gives, in
  * use until the stream has passed the call, and holds nothing before or after it: calls that can run at the same time need one
  * each.  An output overlaps no other argument unless the call says so.  Equal calls give equal bits: no sum depends on timing.
+ * d_status is NULL or the address of one 4-byte aligned device word, into which bits are ORed.  As in the other kernels that wait for
+ * copies and products, a wait within mt_kernel_vocab_loss or its gradient that runs out (after 4 s) leaves the outputs invalid and is told
+ * by MT_FLAG_WAIT_TIMEOUT there and nowhere else: a caller who passes NULL does not learn of it.
  * Errors: UNSUPPORTED (a dtype that is none of those below), SHAPE (negative or too large sizes, strides below the row's
  * length), INVALID_ARG (null or misaligned pointers, a workspace that is too small), CUDA. */
 #define MT_DTYPE_BF16 0

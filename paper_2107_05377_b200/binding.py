@@ -249,6 +249,8 @@ def mt_kernel_pooler_head_static(hidden, pool_w, pool_b, cls_w, cls_b, logits, b
 # ---------------------------------------------------------------------------
 # the vocabulary's ends of a language model, and dropout
 # ---------------------------------------------------------------------------
+# ``status``: one 32-bit word on the device, zeroed by the caller, that a call ORs its FLAG_* bits into (ids and labels outside the
+# vocabulary, waits that ran out and left the outputs invalid).  Calls return before the kernels run, so nothing else tells of them.
 
 class _Torch:
     """What the calls below need of torch, looked up once: a short call spends more time on this side than on the GPU."""

@@ -25,9 +25,9 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortDigitBits = 9;                     // at most
 constexpr int kSortBins = 1 << kSortDigitBits;
 constexpr int kSortMaxCluster = 16;                   // (more than the portable eight)
-// counters of every warp, totals of this CTA (two passes in turn), first places of the digits, warp sums of a scan
 constexpr int kSortUnroll = 8;                        // rounds of a warp whose entries are in registers at a time
 constexpr int kSortAlone = 2048;                      // tokens that one CTA sorts alone, in shared memory
+// counters of every warp, totals of this CTA (two passes in turn), first places of the digits, warp sums of a scan
 constexpr int kSortCountBytes = (kSortWarps * kSortBins + 2 * kSortBins + kSortBins + kSortWarps) * 4;
 constexpr int kSortSmemBytes = kSortCountBytes + kSortAlone * 8;
 constexpr int kSumColumns = 8;                        // columns of a thread

@@ -1,5 +1,5 @@
 """Lookup of rows and the gradient of the table against their definitions in 64 bits: one token to tens of thousands (one CTA to a
-cluster of eight sorts them), one row to more than a million (one to three sort passes), widths that are no multiple of eight,
+cluster of sixteen sorts them), one row to 2^31 - 1 (one to four sort passes), widths that are no multiple of eight,
 rows further apart than they are long, runs of equal ids inside a chunk, over its border and over many chunks."""
 import numpy as np
 import pytest
